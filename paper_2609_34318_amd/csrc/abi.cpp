@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "hydra_attn.h"
+#include "hydra_scores.h"
 #include "kernels.h"
 #include "plan.h"
 #include "prof.h"
@@ -18,6 +19,9 @@ namespace hydra {
 hipError_t launch_attn_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
 hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
                            char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
+hipError_t launch_scores_fwd(const ScoreArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
+hipError_t launch_scores_bwd(const ScoreArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+                             char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
 hipError_t launch_lse_merge(int64_t n_rows, int H, float* o_acc, float* lse_acc, const float* o_part,
                             const float* lse_part, uint16_t* o_bf16, hipStream_t stream);
 }  // namespace hydra
@@ -159,8 +163,9 @@ Launch list_launch(void* ws, size_t whole, int64_t n_whole, const ListSize& l, c
 }
 
 std::vector<int64_t> plan_key(const Problem& pr) {
-  std::vector<int64_t> k = {pr.H, pr.Hkv, int64_t(pr.cu.size())};
+  std::vector<int64_t> k = {pr.H, pr.Hkv, int64_t(pr.cu.size()), int64_t(pr.pe.size())};
   k.insert(k.end(), pr.cu.begin(), pr.cu.end());
+  k.insert(k.end(), pr.pe.begin(), pr.pe.end());
   for (const hydra_chunk_t* c : {&pr.q, &pr.kv}) {
     k.push_back(c->n_segs);
     for (int s = 0; s < c->n_segs; ++s) {
@@ -215,15 +220,30 @@ AttnArgs base_args(const Problem& pr, const WsLayout& w, void* ws) {
   return a;
 }
 
+ScoreArgs score_args(const Problem& pr, const AttnArgs& base) {
+  ScoreArgs a{};
+  static_cast<AttnArgs&>(a) = base;
+  a.pe = base.cu + pr.cu.size();
+  a.slopes = pr.slopes;
+  a.cap = pr.softcap;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
 
-size_t hydra_workspace_size(const hydra_problem_t* p) {
-  Problem pr;
-  if (check_problem(p, &pr) != HYDRA_OK) return 0;
-  return ws_layout(pr).total;
+size_t hydra_scores_workspace_size(const hydra_problem_t* p, const hydra_scores_t* sc) {
+  try {
+    Problem pr;
+    if (check_problem(p, sc, &pr) != HYDRA_OK) return 0;
+    return ws_layout(pr).total;
+  } catch (...) {
+    return 0;
+  }
 }
+
+size_t hydra_workspace_size(const hydra_problem_t* p) { return hydra_scores_workspace_size(p, nullptr); }
 
 }  // extern "C"
 
@@ -231,11 +251,11 @@ namespace {
 
 // Forward of one ring step; `upload` = false launches only (the plan is already in the
 // workspace, from hydra_attn_plan); `merge` = true merges the partial into o_part and lse_part.
-int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_part,
-                  float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, Scratch scratch, void* stream) {
+int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const hydra_scores_t* sc, const void* q,
+                  const void* k, const void* v, float* o_part, float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, Scratch scratch, void* stream) {
   try {
     Problem pr;
-    int rc = check_problem(p, &pr);
+    int rc = check_problem(p, sc, &pr);
     if (rc != HYDRA_OK) return rc;
     if (pr.nq == 0) return HYDRA_OK;
     const bool has_k = pr.nk > 0;
@@ -251,7 +271,7 @@ int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const void*
                    vb = rows_bytes(pr.nk, pr.v_s, pr.Hkv * kDv);
     if (outputs_overlap({{o_part, qh * kDv * 4}, {lse_part, qh * 4}, {o_bf16, qh * kDv * 2}, {workspace, w.total},
                          {scratch.at, scratch.bytes}},
-                        {{q, qb}, {k, kb}, {v, vb}}))
+                        {{q, qb}, {k, kb}, {v, vb}, {pr.slopes, uint64_t(pr.H) * 4}}))
       return HYDRA_ERR_INVALID;
     hipStream_t s = static_cast<hipStream_t>(stream);
     PlanRecord plan;
@@ -270,8 +290,10 @@ int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const void*
     a.out_lse = lse_part;
     a.split = scratch.take(parts_bytes(Kernel::kFwd, plan.fwd, pr.H));
     const Launch l = list_launch(workspace, w.qitems_off, w.n_qitems, plan.fwd, a.split);
-    if (launch_attn_fwd(a, l, static_cast<uint16_t*>(o_bf16), merge, s) != hipSuccess) return HYDRA_ERR_HIP;
-    return HYDRA_OK;
+    uint16_t* b = static_cast<uint16_t*>(o_bf16);
+    const hipError_t e =
+        pr.scored ? launch_scores_fwd(score_args(pr, a), l, b, merge, s) : launch_attn_fwd(a, l, b, merge, s);
+    return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
   } catch (...) {
     return HYDRA_ERR_INVALID;
   }
@@ -285,13 +307,13 @@ uint64_t ds_bytes_per_head(const Problem& pr) {
   return uint64_t(ds_tables(pr, kitems, &kbase, &kmap32, &krec)) * DS_TILE_BYTES;
 }
 
-int attn_bwd_impl(bool upload, const hydra_problem_t* p, const void* q, const void* k, const void* v,
-                  const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
+int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k,
+                  const void* v, const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
                   float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, Scratch scratch,
                   void* stream, bool noalloc = false) {
   try {
     Problem pr;
-    int rc = check_problem(p, &pr);
+    int rc = check_problem(p, sc, &pr);
     if (rc != HYDRA_OK) return rc;
     if (pr.nq == 0 || pr.nk == 0) return HYDRA_OK;
     for (int c : {check_ptr(q, true), check_ptr(k, true), check_ptr(v, true), check_ptr(o_final, true),
@@ -317,7 +339,7 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const void* q, const vo
     if (outputs_overlap({{dq_acc, qh * kDqk * 4}, {dk_acc, kh * kDqk * 4}, {dv_acc, kh * kDv * 4},
                          {workspace, w.total}, {kv_per_pass ? ds_buf : nullptr, ds_used}, {scratch.at, scratch.bytes}},
                         {{q, qb}, {k, kb}, {v, vb}, {o_final, qh * kDv * 2}, {lse_final, qh * 4},
-                         {d_o, qh * kDv * 2}}))
+                         {d_o, qh * kDv * 2}, {pr.slopes, uint64_t(pr.H) * 4}}))
       return HYDRA_ERR_INVALID;
     hipStream_t s = static_cast<hipStream_t>(stream);
     PlanRecord plan;
@@ -347,8 +369,10 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const void* q, const vo
     const Launch q_whole = list_launch(workspace, w.qitems_off, w.n_qitems, ListSize{}, nullptr);
     const Launch dq = list_launch(workspace, w.qitems_off, w.n_qitems, plan.dq, dq_parts);
     const Launch kv = list_launch(workspace, w.kitems_off, w.n_kitems, plan.kv, kv_parts);
-    if (launch_attn_bwd(a, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s) != hipSuccess) return HYDRA_ERR_HIP;
-    return HYDRA_OK;
+    const hipError_t e =
+        pr.scored ? launch_scores_bwd(score_args(pr, a), q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s)
+                  : launch_attn_bwd(a, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s);
+    return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
   } catch (...) {
     return HYDRA_ERR_INVALID;
   }
@@ -358,10 +382,11 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const void* q, const vo
 
 extern "C" {
 
-int hydra_attn_plan(const hydra_problem_t* p, void* workspace, size_t workspace_bytes, void* stream) {
+int hydra_scores_plan(const hydra_problem_t* p, const hydra_scores_t* sc, void* workspace, size_t workspace_bytes,
+                      void* stream) {
   try {
     Problem pr;
-    int rc = check_problem(p, &pr);
+    int rc = check_problem(p, sc, &pr);
     if (rc != HYDRA_OK) return rc;
     const WsLayout w = ws_layout(pr);
     if (!workspace || workspace_bytes < w.total) return HYDRA_ERR_WORKSPACE;
@@ -375,41 +400,61 @@ int hydra_attn_plan(const hydra_problem_t* p, void* workspace, size_t workspace_
   }
 }
 
+int hydra_attn_plan(const hydra_problem_t* p, void* workspace, size_t workspace_bytes, void* stream) {
+  return hydra_scores_plan(p, nullptr, workspace, workspace_bytes, stream);
+}
+
+int hydra_scores_fwd(const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k, const void* v,
+                     float* o, float* lse, void* o_bf16, void* workspace, size_t workspace_bytes, void* scratch,
+                     size_t scratch_bytes, int32_t merge, int32_t planned, void* stream) {
+  return attn_fwd_impl(planned == 0, merge != 0, p, sc, q, k, v, o, lse, o_bf16, workspace, workspace_bytes,
+                       Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
+}
+
+int hydra_scores_bwd(const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k, const void* v,
+                     const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
+                     float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes,
+                     void* scratch, size_t scratch_bytes, int32_t planned, void* stream) {
+  if (planned && ds_buf) return HYDRA_ERR_INVALID;
+  return attn_bwd_impl(planned == 0, p, sc, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+                       workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
+}
+
 int hydra_attn_fwd(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_part,
                    float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_fwd_impl(true, false, p, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
+  return attn_fwd_impl(true, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_fwd_planned(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_part,
                            float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_fwd_impl(false, false, p, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
+  return attn_fwd_impl(false, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_fwd_merge(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_acc,
                          float* lse_acc, void* o_bf16, void* workspace, size_t workspace_bytes, int32_t planned,
                          void* stream) {
-  return attn_fwd_impl(planned == 0, true, p, q, k, v, o_acc, lse_acc, o_bf16, workspace, workspace_bytes, Scratch{},
+  return attn_fwd_impl(planned == 0, true, p, nullptr, q, k, v, o_acc, lse_acc, o_bf16, workspace, workspace_bytes, Scratch{},
                        stream);
 }
 
 int hydra_attn_fwd_split(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o, float* lse,
                          void* o_bf16, void* workspace, size_t workspace_bytes, void* scratch, size_t scratch_bytes,
                          int32_t merge, int32_t planned, void* stream) {
-  return attn_fwd_impl(planned == 0, merge != 0, p, q, k, v, o, lse, o_bf16, workspace, workspace_bytes,
+  return attn_fwd_impl(planned == 0, merge != 0, p, nullptr, q, k, v, o, lse, o_bf16, workspace, workspace_bytes,
                        Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 
 int hydra_attn_bwd(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
                    const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc, float* dv_acc,
                    void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(true, p, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
+  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
                        workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_bwd_ds(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
                       const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc, float* dv_acc,
                       void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(true, p, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
                        workspace, workspace_bytes, Scratch{}, stream);
 }
 
@@ -467,17 +512,17 @@ int hydra_attn_bwd_noalloc(const hydra_problem_t* p, const void* q, const void* 
     if (noalloc_bytes(pr) > kNoAllocLimitBytes) return HYDRA_ERR_TOO_LARGE;
     void* ws = nullptr;
     if ((rc = scratch_ptr(&ws)) != HYDRA_OK) return rc;
-    return attn_bwd_impl(true, p, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, ws,
+    return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, ws,
                          kNoAllocScratchBytes, Scratch{}, stream, true);
   } catch (...) {
     return HYDRA_ERR_INVALID;
   }
 }
 
-size_t hydra_bwd_ds_bytes(const hydra_problem_t* p, int32_t kv_heads_per_pass) {
+size_t hydra_scores_ds_bytes(const hydra_problem_t* p, const hydra_scores_t* sc, int32_t kv_heads_per_pass) {
   try {
     Problem pr;
-    if (check_problem(p, &pr) != HYDRA_OK || kv_heads_per_pass < 1) return 0;
+    if (check_problem(p, sc, &pr) != HYDRA_OK || kv_heads_per_pass < 1) return 0;
     const uint64_t per_head = ds_bytes_per_head(pr);
     return size_t(per_head * uint64_t(std::min(kv_heads_per_pass, pr.Hkv)) * uint64_t(pr.H / pr.Hkv));
   } catch (...) {
@@ -485,10 +530,14 @@ size_t hydra_bwd_ds_bytes(const hydra_problem_t* p, int32_t kv_heads_per_pass) {
   }
 }
 
+size_t hydra_bwd_ds_bytes(const hydra_problem_t* p, int32_t kv_heads_per_pass) {
+  return hydra_scores_ds_bytes(p, nullptr, kv_heads_per_pass);
+}
+
 int hydra_attn_bwd_planned(const hydra_problem_t* p, const void* q, const void* k, const void* v,
                            const void* o_final, const float* lse_final, const void* d_o, float* dq_acc,
                            float* dk_acc, float* dv_acc, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(false, p, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
+  return attn_bwd_impl(false, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
                        workspace_bytes, Scratch{}, stream);
 }
 
@@ -497,18 +546,20 @@ int hydra_attn_bwd_split(const hydra_problem_t* p, const void* q, const void* k,
                          void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, void* scratch,
                          size_t scratch_bytes, int32_t planned, void* stream) {
   if (planned && ds_buf) return HYDRA_ERR_INVALID;
-  return attn_bwd_impl(planned == 0, p, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+  return attn_bwd_impl(planned == 0, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
                        workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 
-size_t hydra_split_scratch_size(const hydra_problem_t* p) {
+size_t hydra_scores_scratch_size(const hydra_problem_t* p, const hydra_scores_t* sc) {
   try {
     Problem pr;
-    return check_problem(p, &pr) == HYDRA_OK ? size_t(split_scratch_bytes(pr)) : 0;
+    return check_problem(p, sc, &pr) == HYDRA_OK ? size_t(split_scratch_bytes(pr)) : 0;
   } catch (...) {
     return 0;
   }
 }
+
+size_t hydra_split_scratch_size(const hydra_problem_t* p) { return hydra_scores_scratch_size(p, nullptr); }
 
 int hydra_lse_merge(int64_t n_rows, int32_t n_heads, int32_t d_v, float* o_acc, float* lse_acc,
                     const float* o_part, const float* lse_part, void* o_out_bf16, void* stream) {
@@ -543,24 +594,38 @@ const char* hydra_strerror(int status) {
   }
 }
 
-int64_t hydra_visible_pairs(const hydra_problem_t* p) {
-  Problem pr;
-  if (check_problem(p, &pr) != HYDRA_OK) return -1;
-  return visible_pairs(pr);
+int64_t hydra_scores_visible_pairs(const hydra_problem_t* p, const hydra_scores_t* sc) {
+  try {
+    Problem pr;
+    return check_problem(p, sc, &pr) == HYDRA_OK ? visible_pairs(pr) : -1;
+  } catch (...) {
+    return -1;
+  }
+}
+
+int64_t hydra_visible_pairs(const hydra_problem_t* p) { return hydra_scores_visible_pairs(p, nullptr); }
+
+int64_t hydra_scores_plan_items(const hydra_problem_t* p, const hydra_scores_t* sc, int32_t which, int32_t* out,
+                                int64_t cap) {
+  try {
+    Problem pr;
+    int rc = check_problem(p, sc, &pr);
+    if (rc != HYDRA_OK) return rc;
+    if (which != 0 && which != 1) return HYDRA_ERR_INVALID;
+    if (cap < 0 || (cap > 0 && !out)) return HYDRA_ERR_INVALID;
+    std::vector<int32_t> items;
+    plan_items(pr, which, &items);
+    const int64_t n = int64_t(items.size()) / kItemInts;
+    const int64_t k = n < cap ? n : cap;
+    if (k > 0) std::memcpy(out, items.data(), size_t(k) * kItemInts * sizeof(int32_t));
+    return n;
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
+  }
 }
 
 int64_t hydra_plan_items(const hydra_problem_t* p, int32_t which, int32_t* out, int64_t cap) {
-  Problem pr;
-  int rc = check_problem(p, &pr);
-  if (rc != HYDRA_OK) return rc;
-  if (which != 0 && which != 1) return HYDRA_ERR_INVALID;
-  if (cap < 0 || (cap > 0 && !out)) return HYDRA_ERR_INVALID;
-  std::vector<int32_t> items;
-  plan_items(pr, which, &items);
-  const int64_t n = int64_t(items.size()) / kItemInts;
-  const int64_t k = n < cap ? n : cap;
-  if (k > 0) std::memcpy(out, items.data(), size_t(k) * kItemInts * sizeof(int32_t));
-  return n;
+  return hydra_scores_plan_items(p, nullptr, which, out, cap);
 }
 
 int hydra_profile_start(void) {

@@ -11,8 +11,13 @@
 // deterministic: every output row is owned by exactly one workgroup.  Both kinds
 // stream their other-side tiles through swizzled LDS stages filled by direct
 // buffer->LDS copies issued ahead of use.
+//
+// MOD: modified scores (hydra_scores.h, scores.h); kPlain is the attention of hydra_attn.h.  A cap multiplies
+// dS by 1 - tanh^2: the dQ workgroups multiply it into dP - D, role A of dK/dV into the P that it
+// hands to role B, which needs no other.
 #include "kernels.h"
 #include "prof.h"
+#include "scores.h"
 
 namespace hydra {
 
@@ -69,7 +74,7 @@ __device__ __forceinline__ void dq_issue(lds_char* stage, const AttnArgs& a, con
 constexpr int DQ_LDS = DQ_STAGE + DQ_WAVES * own_bytes<DQK>();
 static_assert(DQ_LDS >= DQ_NSTAGE * DQ_STAGE && DQ_LDS >= DQ_WAVES * ROWS_OUT_BYTES, "LDS");
 
-__device__ __forceinline__ void bwd_dq_body(const AttnArgs& a, int block, lds_char* smem) {
+template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& a, int block, lds_char* smem) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // wave-uniform, known to the compiler
   const int m = lane & 31;
@@ -96,9 +101,21 @@ __device__ __forceinline__ void bwd_dq_body(const AttnArgs& a, int block, lds_ch
   const int mc = q_n > 0 ? min(m, q_n - 1) : -32 * wave;
   float lse2 = a.lse2[(int64_t)head * a.nq + q_row0 + mc];
   float neg_D = a.Dvec[(int64_t)head * a.nq + q_row0 + mc];
-  const int lo_q = doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, q_pos0 + mc);
+  int lo_q, hi_row = 0, hi_first, hi_last;  // as in the forward; hi_row: of this lane's row
+  if constexpr (MOD != kPlain) {
+    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, q_pos0 + mc);
+    lo_q = see.lo;
+    hi_row = see.hi;
+    hi_first = __builtin_amdgcn_readfirstlane(see.hi);
+    hi_last = q_n > 0 ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
+  } else {
+    lo_q = doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, q_pos0 + mc);
+    hi_first = q_pos0 + 1;
+    hi_last = q_last + 1;
+  }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
+  const ScoreConst sc = score_const<MOD>(a, head);
   settle(lse2);
   settle(neg_D);
   bf16x8 qf[DQK / 16], df[DV / 16];
@@ -130,8 +147,8 @@ __device__ __forceinline__ void bwd_dq_body(const AttnArgs& a, int block, lds_ch
       dq_issue(smem + ((t + 1) % DQ_NSTAGE) * DQ_STAGE, a, cur, kv_head, wave);
     }
     // a wave none of whose rows sees the tile leaves the matrix cores to the others
-    if (kpos > q_last || kpos + kn <= lo_first) continue;
-    const bool full = (kn == DQ_BK) && (lo_last <= kpos) && (kpos + DQ_BK - 1 <= q_pos0);
+    if (kpos >= hi_last || kpos + kn <= lo_first) continue;
+    const bool full = (kn == DQ_BK) && (lo_last <= kpos) && (kpos + DQ_BK <= hi_first);
 
     static_for<DQ_BK / 32>([&](auto kb_) {
       constexpr int kb = decltype(kb_)::value;
@@ -142,22 +159,30 @@ __device__ __forceinline__ void bwd_dq_body(const AttnArgs& a, int block, lds_ch
       for (int t2 = 0; t2 < DV / 16; ++t2) dp = mfma(op_b128<DQ_BK>(Vs, o, 32 * kb, t2), df[t2], dp);
 
       float ds[16];
+      if constexpr (in_log2<MOD>()) {
+        const int ml = lane_now();
+        score16_grad<MOD, -1>(s, sc, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)),
+                              [&](int e, float f) { dp[e] = (dp[e] + neg_D) * f; });
+      }
+      // exponent of P, and (dP - D) with the cap's factor
+      auto arg = [&](int e) { return in_log2<MOD>() ? s[e] - lse2 : __builtin_fmaf(s[e], sl2, -lse2); };
+      auto dpd = [&](int e) { return (MOD & kCap) ? dp[e] : dp[e] + neg_D; };
       if (full) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse2)) * (dp[e] + neg_D);
+        for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(arg(e)) * dpd(e);
       } else {
-        // key kpos + key(e) is visible iff lo_q <= it <= pos_q and key(e) < kn, i.e. iff
+        // key kpos + key(e) is visible iff lo_q <= it < hi_q and key(e) < kn, i.e. iff
         // 0 <= base + c(e) < lim with base = kpos - lo_q + 32*kb + 8*hh; masked entries get
-        // exp2(-inf) = 0.  pos_q is formed here: this kernel has no register to spare for it.
+        // exp2(-inf) = 0.  hi_q is formed here: this kernel has no register to spare for it.
         const int ml = lane_now();
-        const int pos_q = (ml & 31) < q_n ? q_pos0 + (ml & 31) : -1;
+        const int hi_q = (ml & 31) < q_n ? (MOD != kPlain ? hi_row : q_pos0 + (ml & 31) + 1) : 0;
         const int base = kpos - lo_q + 32 * kb + 8 * (ml >> 5);
-        const int lim = max(0, min(pos_q + 1, kpos + kn) - lo_q);
+        const int lim = max(0, min(hi_q, kpos + kn) - lo_q);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int r = base + 16 * (e >> 3) + (e & 7);
           const bool vis = (unsigned)r < (unsigned)lim;
-          ds[e] = __builtin_amdgcn_exp2f(vis ? __builtin_fmaf(s[e], sl2, -lse2) : -INFINITY) * (dp[e] + neg_D);
+          ds[e] = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY) * dpd(e);
         }
       }
       const bf16x8 dsf[2] = {to_bf16x8(ds), to_bf16x8(ds + 8)};
@@ -251,8 +276,8 @@ __device__ __forceinline__ void kv_clear_tail(lds_char* stage, int n, int wave_b
 
 // STORE_DS: also store dS (bf16, as the MFMA operand registers hold it) for the query-
 // stationary dQ kernel that reads it back instead of recomputing S and dP.
-template <bool STORE_DS>
-__device__ __forceinline__ void bwd_dkdv_body(const AttnArgs& a, int block, lds_char* smem) {
+template <bool STORE_DS, int MOD>
+__device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds_char* smem) {
   lds_char* pbuf = smem + KV_NSTAGE * KV_STAGE;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -273,10 +298,22 @@ __device__ __forceinline__ void bwd_dkdv_body(const AttnArgs& a, int block, lds_
 
   const int kj = pair * 32 + m;
   const bool k_valid = kj < k_n;
-  const int pos_k = k_valid ? k_pos0 + kj : 0x7fffffff;
-  const int hi_k = doc_edge<true>(a.cu, it.d0, it.d1, it.edge0, k_pos0 + min(kj, k_n - 1));
   const int kn_w = min(32, max(0, k_n - pair * 32));  // valid keys of this pair
-  const int wk_first = k_pos0 + pair * 32, wk_last = wk_first + kn_w - 1;
+  // queries at [lo_k, hi_k) see this lane's key (lanes past the end: none), those from lo_first on the
+  // pair's first one and those from lo_last on its last
+  int lo_k, hi_k, lo_first, lo_last;
+  if constexpr (MOD != kPlain) {
+    const Span seen = row_span<true>(a.cu, a.pe, it.d0, it.d1, k_pos0 + min(kj, k_n - 1));
+    lo_k = k_valid ? seen.lo : 0x7fffffff;
+    hi_k = seen.hi;
+    lo_first = __builtin_amdgcn_readfirstlane(seen.lo);
+    lo_last = __builtin_amdgcn_readlane(seen.lo, 31);
+  } else {
+    lo_k = k_valid ? k_pos0 + kj : 0x7fffffff;
+    hi_k = doc_edge<true>(a.cu, it.d0, it.d1, it.edge0, k_pos0 + min(kj, k_n - 1));
+    lo_first = k_pos0 + pair * 32;
+    lo_last = lo_first + kn_w - 1;
+  }
   // document ends of the pair's first and last key (lanes past the end repeat the last one)
   const int hi_first = __builtin_amdgcn_readfirstlane(hi_k);
   const int hi_last = __builtin_amdgcn_readlane(hi_k, 31);
@@ -323,12 +360,13 @@ __device__ __forceinline__ void bwd_dkdv_body(const AttnArgs& a, int block, lds_
     for (int t = 0; t < n_tiles; ++t) {
       refresh(o);
       const int qpos = cur.q.pos0, qn = cur.q.n;
+      const ScoreConst score_c = score_const<MOD>(a, head0 + cur.member);  // the slope is the query head's
       const int64_t ds_off = (int64_t)(ds_head0 + cur.member) * a.ds_head_bytes +
                              (int64_t)(ds_slot0 + cur.qt) * DS_TILE_BYTES;  // this tile's dS slot
       const bool more = t + 1 < n_tiles;
       if (more) cur = kv_next(qr, cur);
       // a pair whose keys no row of the tile sees leaves the matrix cores to the others
-      const bool sees = active && qpos + qn > wk_first && qpos < hi_last;
+      const bool sees = active && qpos + qn > lo_first && qpos < hi_last;
       if constexpr (ROLE == 1) {
         wait_dma();  // tile t's copies, the only ones in flight
         if (qn < KV_BQ) kv_clear_tail(smem + (t % KV_NSTAGE) * KV_STAGE, qn, pair, lane_now());
@@ -367,34 +405,49 @@ __device__ __forceinline__ void bwd_dkdv_body(const AttnArgs& a, int block, lds_
           static_for<KV_BQ / 32>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
             const int qb = qpos + 32 * sb;
-            const f32x16& s = sc[sb];
+            f32x16& s = sc[sb];
             // this lane's query rows are 32*sb + 8*hh + {0..7, 16..23}
             f32x4 l0, l1, l2, l3;
             lds_x4_f32<128 * sb, 128 * sb + 16, 128 * sb + 64, 128 * sb + 80>(vec_s, 32 * hh, l0, l1, l2, l3);
             const float lse_r[16] = {l0[0], l0[1], l0[2], l0[3], l1[0], l1[1], l1[2], l1[3],
                                      l2[0], l2[1], l2[2], l2[3], l3[0], l3[1], l3[2], l3[3]};
-            const bool full = (kn_w == 32) && (qn >= 32 * (sb + 1)) && (wk_last <= qb) && (qb + 31 < hi_first);
-            float p[16];
+            const bool full = (kn_w == 32) && (qn >= 32 * (sb + 1)) && (lo_last <= qb) && (qb + 31 < hi_first);
+            float p[16], f[16];
+            if constexpr (in_log2<MOD>()) {
+              const int ml = lane_now();
+              score16_grad<MOD, 1>(s, score_c, float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31))),
+                                   [&](int e, float g) { f[e] = g; });
+            }
+            auto arg = [&](int e) {
+              return in_log2<MOD>() ? s[e] - lse_r[e] : __builtin_fmaf(s[e], sl2, -lse_r[e]);
+            };
             if (full) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse_r[e]));
+              for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(arg(e));
             } else {
               // query row qq = base + c(e) is visible iff lo <= base + c(e) < lim, where base
-              // is this lane's first row relative to its key position; masked entries get
+              // is this lane's first row relative to the first that sees its key; masked entries get
               // exp2(-inf)
-              const int base = qpos - pos_k + 32 * sb + 8 * hh;
-              const int lim = max(0, min(qpos + qn, hi_k) - pos_k);
+              const int base = qpos - lo_k + 32 * sb + 8 * hh;
+              const int lim = max(0, min(qpos + qn, hi_k) - lo_k);
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const int r = base + 16 * (e >> 3) + (e & 7);
                 const bool vis = (unsigned)r < (unsigned)lim;
-                p[e] = __builtin_amdgcn_exp2f(vis ? __builtin_fmaf(s[e], sl2, -lse_r[e]) : -INFINITY);
+                p[e] = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY);
               }
             }
             pk[2 * sb] = to_bf16x8(p);
             pk[2 * sb + 1] = to_bf16x8(p + 8);
-            lds_st16<2048 * sb>(pbuf, poff, pk[2 * sb]);
-            lds_st16<2048 * sb + 1024>(pbuf, poff, pk[2 * sb + 1]);
+            if constexpr (MOD & kCap) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) p[e] *= f[e];
+              lds_st16<2048 * sb>(pbuf, poff, to_bf16x8(p));
+              lds_st16<2048 * sb + 1024>(pbuf, poff, to_bf16x8(p + 8));
+            } else {
+              lds_st16<2048 * sb>(pbuf, poff, pk[2 * sb]);
+              lds_st16<2048 * sb + 1024>(pbuf, poff, pk[2 * sb + 1]);
+            }
           });
         }
         barrier_lds();  // P of this tile is in LDS
@@ -511,9 +564,9 @@ __device__ __forceinline__ void bwd_dkdv_body(const AttnArgs& a, int block, lds_
   else run(IntC<1>{});
 }
 
-__global__ __launch_bounds__(512, 1) void bwd_dkdv_ds_kernel(AttnArgs a) {
+template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dkdv_ds_kernel(Args<MOD> a) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[KV_LDS];
-  bwd_dkdv_body<true>(a, blockIdx.x, (lds_char*)smem_raw);
+  bwd_dkdv_body<true, MOD>(a, blockIdx.x, (lds_char*)smem_raw);
 }
 
 // The recompute backward: dK/dV, then dQ, in one launch.  The workgroups of dQ, which needs nothing
@@ -524,13 +577,13 @@ __global__ __launch_bounds__(512, 1) void bwd_dkdv_ds_kernel(AttnArgs a) {
 // 32K and 64K rows in one document (21.6 ms, 84 ms).  The two lists interleaved, both walked to
 // the end together, lost where workgroups are long (64K: 79.3 to 83.2 ms): dK/dV's and dQ's tiles then
 // share the L2s.  Up to seven places after dK/dV stay empty, so that dQ's heads keep their XCDs.
-__global__ __launch_bounds__(512, 1) void bwd_recompute_kernel(AttnArgs q, AttnArgs kv) {
+template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_recompute_kernel(Args<MOD> q, Args<MOD> kv) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[DQ_LDS > KV_LDS ? DQ_LDS : KV_LDS];
   lds_char* smem = (lds_char*)smem_raw;
   const int nkv = kv.n_items * kv.kv_heads;
   const int b = blockIdx.x, q0 = (nkv + N_XCD - 1) / N_XCD * N_XCD;
-  if (b < nkv) bwd_dkdv_body<false>(kv, b, smem);
-  else if (b >= q0) bwd_dq_body(q, b - q0, smem);
+  if (b < nkv) bwd_dkdv_body<false, MOD>(kv, b, smem);
+  else if (b >= q0) bwd_dq_body<MOD>(q, b - q0, smem);
 }
 
 // ------------------------------------------------------------------ dQ from stored dS
@@ -564,7 +617,7 @@ struct DsTile {
 // flight, as vector loads after the copies' memory-clobbering assembly would be).
 struct DsWalk {
   int rr, r, end, kpos_r, j;  // range, next key row, the range's end, key position - key row, record
-  int lo_first, q_last;       // document start of the wave's first row, position of its last (-1: no rows)
+  int lo_first, hi_last;      // first position that the wave's first row sees, one past its last row's last (0: no rows)
   i32x16 rec;
 };
 
@@ -604,7 +657,7 @@ __device__ __forceinline__ DsTile ds_next(const AttnArgs& a, const DsRanges R, D
   // the sub-block of the item's query tiling that holds the wave's rows [qrow, qrow + 32)
   d.off = -1;
   const int kpos = d.krow0 + w.kpos_r;  // a key item lies in one segment: its rows' positions are consecutive
-  if (kpos <= w.q_last && kpos + d.kn > w.lo_first) {
+  if (kpos < w.hi_last && kpos + d.kn > w.lo_first) {
     int slot = w.rec[3];
 #pragma unroll
     for (int k = 0; k < MAX_RANGES; ++k) {
@@ -622,7 +675,8 @@ __device__ __forceinline__ DsTile ds_next(const AttnArgs& a, const DsRanges R, D
   return d;
 }
 
-__global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(AttnArgs a) {
+// MOD: kPlain or kScored; what else the scores have lies in the stored dS.
+template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Args<MOD> a) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[DQS_LDS];
   lds_char* smem = (lds_char*)smem_raw;
   lds_char* dsmem = smem + DQS_KSTAGES * DQS_KBYTES;
@@ -643,9 +697,15 @@ __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(AttnArgs a) {
   walk.rr = -1;
   walk.r = 0;
   walk.end = 0;
-  walk.q_last = wave_rows ? it.pos0 + 32 * wave + 31 : -1;
-  walk.lo_first = __builtin_amdgcn_readfirstlane(
-      doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, it.pos0 + (wave_rows ? 32 * wave : 0)));
+  if constexpr (MOD != kPlain) {
+    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, it.pos0 + (wave_rows ? 32 * wave + m : 0));
+    walk.lo_first = __builtin_amdgcn_readfirstlane(see.lo);
+    walk.hi_last = wave_rows ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
+  } else {
+    walk.hi_last = wave_rows ? it.pos0 + 32 * wave + 32 : 0;
+    walk.lo_first = __builtin_amdgcn_readfirstlane(
+        doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, it.pos0 + (wave_rows ? 32 * wave : 0)));
+  }
   DsTile t0 = ds_next(a, R, walk, qrow0);
   if (!t0.valid) return;  // uniform over the workgroup
   const int kv_head = head / a.grp;
@@ -779,8 +839,8 @@ __global__ __launch_bounds__(64) void bwd_merge_kernel(AttnArgs q, AttnArgs kv, 
 namespace {
 
 // a over a list, whose parts lie at split.
-AttnArgs list_args(const AttnArgs& a, const Launch& l, char* split) {
-  AttnArgs b = a;
+template <class A> A list_args(const A& a, const Launch& l, char* split) {
+  A b = a;
   b.items = l.units;
   b.n_items = l.n_units;
   b.merges = l.merges;
@@ -789,8 +849,8 @@ AttnArgs list_args(const AttnArgs& a, const Launch& l, char* split) {
   return b;
 }
 
-template <class K>
-hipError_t launch_list(K kernel, const char* name, const AttnArgs& a, int heads, hipStream_t stream) {
+template <class K, class A>
+hipError_t launch_list(K kernel, const char* name, const A& a, int heads, hipStream_t stream) {
   if (a.n_items == 0) return hipSuccess;
   const int tok = prof_begin(name, stream);
   hipLaunchKernelGGL(kernel, dim3(a.n_items * heads), dim3(512), 0, stream, a);
@@ -808,25 +868,26 @@ hipError_t launch_merges(const AttnArgs& q, int n_q, const AttnArgs& kv, int n_k
   return hipGetLastError();
 }
 
-hipError_t launch_recompute(const AttnArgs& q, int q_merges, const AttnArgs& kv, int kv_merges, hipStream_t stream) {
+template <int MOD>
+hipError_t launch_recompute(const Args<MOD>& q, int q_merges, const Args<MOD>& kv, int kv_merges, hipStream_t stream) {
   const int64_t nq = (int64_t)q.n_items * q.q_heads, nkv = (int64_t)kv.n_items * kv.kv_heads;
   if (nq + nkv == 0) return hipSuccess;
-  const int tok = prof_begin("bwd_recompute", stream);
+  const int tok = prof_begin(MOD == kPlain ? "bwd_recompute" : "bwd_recompute_scores", stream);
   const int64_t kv_blocks = nq > 0 ? (nkv + N_XCD - 1) / N_XCD * N_XCD : nkv;
-  hipLaunchKernelGGL(bwd_recompute_kernel, dim3(unsigned(kv_blocks + nq)), dim3(512), 0, stream, q, kv);
+  hipLaunchKernelGGL(bwd_recompute_kernel<MOD>, dim3(unsigned(kv_blocks + nq)), dim3(512), 0, stream, q, kv);
   prof_end(tok, stream);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   return launch_merges(q, q_merges, kv, kv_merges, stream);
 }
 
-}  // namespace
-
 // kv_heads_per_pass = 0: recompute path over all heads.  kv_parts, dq_parts: where the parts of dK/dV
 // and dQ go, for a list that has any.
 // Otherwise the stored-dS path, in passes of that many K/V heads (the dS of one pass's query heads
 // fits a.ds): bwd_dkdv_ds stores dS, then bwd_dq_ds reads it back.
-hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                           char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+template <int MOD>
+hipError_t launch_bwd(const Args<MOD>& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+                      char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+  constexpr bool plain = MOD == kPlain;
   const int64_t pairs = (int64_t)a.nq * a.H;
   const int64_t blocks = (pairs + 15) / 16 < (1 << 20) ? (pairs + 15) / 16 : (1 << 20);
   int tok = prof_begin("bwd_pre", stream);
@@ -839,29 +900,45 @@ hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launc
     if (q_whole.n_units == 0 || kv.n_units == 0) return hipSuccess;
     for (int g0 = 0; g0 < a.Hkv; g0 += kv_heads_per_pass) {
       const int G = min(kv_heads_per_pass, a.Hkv - g0);
-      AttnArgs b = list_args(a, kv, kv_parts);
+      Args<MOD> b = list_args(a, kv, kv_parts);
       b.kv_head0 = g0;
       b.kv_heads = G;
       b.q_head0 = g0 * a.grp;
       b.q_heads = G * a.grp;
-      if ((e = launch_list(bwd_dkdv_ds_kernel, "bwd_dkdv_ds", b, G, stream)) != hipSuccess) return e;
-      if ((e = launch_merges(b, 0, b, kv.n_merges, stream)) != hipSuccess) return e;
-      if ((e = launch_list(bwd_dq_ds_kernel, "bwd_dq_ds", list_args(b, q_whole, nullptr), G * a.grp, stream)) !=
+      if ((e = launch_list(bwd_dkdv_ds_kernel<MOD>, plain ? "bwd_dkdv_ds" : "bwd_dkdv_ds_scores", b, G, stream)) !=
           hipSuccess)
+        return e;
+      if ((e = launch_merges(b, 0, b, kv.n_merges, stream)) != hipSuccess) return e;
+      if ((e = launch_list(bwd_dq_ds_kernel<plain ? kPlain : kScored>, plain ? "bwd_dq_ds" : "bwd_dq_ds_scores",
+                           list_args(b, q_whole, nullptr), G * a.grp, stream)) != hipSuccess)
         return e;
     }
     return hipSuccess;
   }
   // a dispatch holds fewer than 2^32 lanes
   const bool turns = (int64_t)dq.n_units * a.H + (int64_t)kv.n_units * a.Hkv + N_XCD > (1 << 23);
-  const AttnArgs q_args = list_args(a, dq, dq_parts), kv_args = list_args(a, kv, kv_parts);
+  const Args<MOD> q_args = list_args(a, dq, dq_parts), kv_args = list_args(a, kv, kv_parts);
   if (turns) {
-    AttnArgs none = a;
+    Args<MOD> none = a;
     none.n_items = 0;
-    if ((e = launch_recompute(none, 0, kv_args, kv.n_merges, stream)) != hipSuccess) return e;
-    return launch_recompute(q_args, dq.n_merges, none, 0, stream);
+    if ((e = launch_recompute<MOD>(none, 0, kv_args, kv.n_merges, stream)) != hipSuccess) return e;
+    return launch_recompute<MOD>(q_args, dq.n_merges, none, 0, stream);
   }
-  return launch_recompute(q_args, dq.n_merges, kv_args, kv.n_merges, stream);
+  return launch_recompute<MOD>(q_args, dq.n_merges, kv_args, kv.n_merges, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+                           char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+  return launch_bwd<kPlain>(a, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
+}
+
+hipError_t launch_scores_bwd(const ScoreArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+                             char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+  return with_mod(a, [&](auto mod) {
+    return launch_bwd<decltype(mod)::value>(a, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
+  });
 }
 
 }  // namespace hydra

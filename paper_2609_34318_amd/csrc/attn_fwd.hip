@@ -15,8 +15,11 @@
 // exp2(s - m) for the same m in numerator and denominator, so the result is unchanged up to
 // rounding (terms stay <= 2^8).  Only tiles that straddle a document start, the causal
 // diagonal or the end of a range evaluate the mask (Sec. 2.2).
+//
+// MOD: modified scores (hydra_scores.h, scores.h); kPlain is the attention of hydra_attn.h.
 #include "kernels.h"
 #include "prof.h"
+#include "scores.h"
 
 namespace hydra {
 
@@ -93,8 +96,8 @@ __device__ __forceinline__ void fwd_out(const AttnArgs& a, uint16_t* o_bf16, lds
   });
 }
 
-template <bool MERGE>
-__global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a, uint16_t* __restrict__ o_bf16) {
+template <bool MERGE, int MOD>
+__global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a, uint16_t* __restrict__ o_bf16) {
   // stage 0 | stage 1; before the loop the waves' Q rows from the start of stage 1, after it
   // their outputs
   constexpr int LDS_BYTES = FWD_STAGE + FWD_WAVES * own_bytes<DQK>();
@@ -128,10 +131,25 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a,
   Tile cur = tile_at(kr, t0, FWD_BK);  // with no tile: of no rows
   fwd_issue(smem, a, cur, koff, voff, wave);
 
-  // document starts: of this lane's row, of the wave's first and last row
-  const int lo_q = doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, q_pos0 + min(m, max(q_n, 1) - 1));
+  // the first position that this lane's row, the wave's first and its last row see (rows past the end
+  // repeat the last one), and the one past their last
+  int lo_q, hi_q, hi_first, hi_last;
+  const int row_pos = q_pos0 + min(m, max(q_n, 1) - 1);
+  if constexpr (MOD != kPlain) {
+    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, row_pos);
+    lo_q = see.lo;
+    hi_first = __builtin_amdgcn_readfirstlane(see.hi);
+    hi_last = q_n > 0 ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
+    hi_q = q_valid ? see.hi : 0;
+  } else {
+    lo_q = doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, row_pos);
+    hi_first = q_pos0 + 1;
+    hi_last = q_last + 1;
+    hi_q = pos_q + 1;
+  }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
-  const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);  // rows past the end repeat the last one
+  const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
+  const ScoreConst sc = score_const<MOD>(a, head);
   bf16x8 qf[DQK / 16];
   wait_dma();
   own_rows_read<DQK>(qbuf, lane, qf);
@@ -157,7 +175,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a,
     }
     // a wave none of whose rows sees the tile (the diagonal's upper half, another document)
     // leaves the matrix cores to the others
-    if (kpos > q_last || kpos + kn <= lo_first) continue;
+    if (kpos >= hi_last || kpos + kn <= lo_first) continue;
 
     f32x16 s[2];
 #pragma unroll
@@ -178,14 +196,19 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a,
     }
     __builtin_amdgcn_sched_group_barrier(0x008, FWD_AHEAD, 0);
 
+    if constexpr (in_log2<MOD>()) {
+      const float d0 = float(q_pos0 + m - kpos - 8 * hh);  // distance of the lane's first key
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) score16<MOD, -1>(s[kb], sc, d0 - 32 * kb);
+    }
     // per wave: in a window of short documents most 256-row tiles straddle a boundary, their
     // 32-row waves seldom
-    const bool full = (kn == FWD_BK) && (lo_last <= kpos) && (kpos + FWD_BK - 1 <= q_pos0);
+    const bool full = (kn == FWD_BK) && (lo_last <= kpos) && (kpos + FWD_BK <= hi_first);
     if (!full) {
-      // key kpos + key(e) is visible iff lo_q <= it <= pos_q and key(e) < kn, i.e. iff
+      // key kpos + key(e) is visible iff lo_q <= it < hi_q and key(e) < kn, i.e. iff
       // 0 <= base + c(e) < lim with base = kpos - lo_q + 8*hh
       const int base = kpos - lo_q + 8 * hh;
-      const int lim = max(0, min(pos_q + 1, kpos + kn) - lo_q);
+      const int lim = max(0, min(hi_q, kpos + kn) - lo_q);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -209,7 +232,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a,
     mx = fmax2(fmax2(mx, mx4[1]), s[1][7]);
     mx = fmax2(fmax2(mx, mx4[2]), s[1][15]);
     mx = fmax2(mx, mx4[3]);
-    const float mxs = xhalf_max(mx) * sl2;  // -inf when nothing is visible
+    const float mxs = xhalf_max(mx) * (in_log2<MOD>() ? 1.0f : sl2);  // -inf when nothing is visible
     if (__builtin_amdgcn_ballot_w64(mxs > m_run + RESCALE_SLACK) != 0) {
       const float m_new = mxs > m_run + RESCALE_SLACK ? mxs : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -227,7 +250,10 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(AttnArgs a,
     for (int j = 0; j < 4; ++j) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 1][8 * (j & 1) + e], sl2, neg_m));
+      for (int e = 0; e < 8; ++e) {
+        const float x = s[j >> 1][8 * (j & 1) + e];
+        p[e] = __builtin_amdgcn_exp2f(in_log2<MOD>() ? x + neg_m : __builtin_fmaf(x, sl2, neg_m));
+      }
       l_run[j] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       pf[j] = to_bf16x8(p);
     }
@@ -293,10 +319,10 @@ __global__ __launch_bounds__(128) void fwd_merge_kernel(AttnArgs a, uint16_t* __
     fwd_out<MERGE, 1, 1>(a, o_bf16, obuf, head, q_row0, q_n, lane, acc, m, l, old_lse);
 }
 
-template <bool MERGE>
-hipError_t launch_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, hipStream_t stream) {
-  int tok = prof_begin("attn_fwd", stream);
-  hipLaunchKernelGGL(attn_fwd_kernel<MERGE>, dim3(a.n_items * a.H), dim3(64 * FWD_WAVES), 0, stream, a, o_bf16);
+template <bool MERGE, int MOD>
+hipError_t launch_fwd(const Args<MOD>& a, const Launch& l, uint16_t* o_bf16, hipStream_t stream) {
+  int tok = prof_begin(MOD == kPlain ? "attn_fwd" : "attn_fwd_scores", stream);
+  hipLaunchKernelGGL((attn_fwd_kernel<MERGE, MOD>), dim3(a.n_items * a.H), dim3(64 * FWD_WAVES), 0, stream, a, o_bf16);
   prof_end(tok, stream);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || l.n_merges == 0) return e;
   tok = prof_begin("attn_fwd_merge", stream);
@@ -306,14 +332,23 @@ hipError_t launch_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, hipS
 }
 
 // merge: into the O and LSE that a.out_o and a.out_lse hold.
-hipError_t launch_attn_fwd(const AttnArgs& args, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream) {
+template <int MOD>
+hipError_t launch_list(const Args<MOD>& args, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream) {
   if (l.n_units == 0) return hipSuccess;
-  AttnArgs a = args;
+  Args<MOD> a = args;
   a.items = l.units;
   a.n_items = l.n_units;
   a.merges = l.merges;
   a.n_parts = l.parts;
-  return merge ? launch_fwd<true>(a, l, o_bf16, stream) : launch_fwd<false>(a, l, o_bf16, stream);
+  return merge ? launch_fwd<true, MOD>(a, l, o_bf16, stream) : launch_fwd<false, MOD>(a, l, o_bf16, stream);
+}
+
+hipError_t launch_attn_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream) {
+  return launch_list<kPlain>(a, l, o_bf16, merge, stream);
+}
+
+hipError_t launch_scores_fwd(const ScoreArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream) {
+  return with_mod(a, [&](auto mod) { return launch_list<decltype(mod)::value>(a, l, o_bf16, merge, stream); });
 }
 
 }  // namespace hydra

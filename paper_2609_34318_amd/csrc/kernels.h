@@ -706,6 +706,20 @@ struct AttnArgs {
   const int* merges;
 };
 
+// ... with modified scores (hydra_scores.h)
+struct ScoreArgs : AttnArgs {
+  const int* pe;        // prefix end of each document
+  const float* slopes;  // [H], or null
+  float cap;            // 0: none
+};
+
+// What a kernel does to its scores: nothing (the plain kernels), or kScored (the prefix mask) with any of
+// the others.
+enum Mod { kPlain = 0, kScored = 1, kCap = 2, kBias = 4 };
+template <int MOD> struct ArgsFor { typedef ScoreArgs type; };
+template <> struct ArgsFor<kPlain> { typedef AttnArgs type; };
+template <int MOD> using Args = typename ArgsFor<MOD>::type;
+
 // Part `part` of the launch's head `hl`.
 __device__ __forceinline__ char* part_at(const AttnArgs& a, int hl, int part, int part_bytes) {
   return a.split + ((int64_t)hl * a.n_parts + part) * part_bytes;

@@ -7,7 +7,9 @@
 // grow with p.  Symmetrically, a key tile [a, b] is seen by the query interval
 // [a, doc_end(b) - 1].  Intersecting that interval with each segment of the other chunk
 // gives at most HYDRA_MAX_SEGS contiguous ranges of local rows; anything outside them is
-// masked (Sec. 2.2) and is never visited.  Tiles are ordered heaviest first, the
+// masked (Sec. 2.2) and is never visited.  With prefixes a row at p of document d sees
+// [doc_start(d), max(p + 1, prefix end(d))), whose ends grow with p too: the intervals end at the last row's
+// prefix where that is later, and a key tile that starts in a prefix is seen from its document's start.  Tiles are ordered heaviest first, the
 // kernel-level counterpart of the scheduler placing the longest sequences first
 // (Sec. 5.1.1, Alg. 1, phase 2).
 #include "plan.h"
@@ -152,6 +154,24 @@ int check_problem(const hydra_problem_t* p, Problem* out) {
   return HYDRA_OK;
 }
 
+int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out) {
+  const int rc = check_problem(p, out);
+  if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len)) return rc;
+  // beyond these the cap's square or the score in units of it leaves the 32-bit range for ordinary inputs
+  if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p14f)) return HYDRA_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(sc->slopes) % sizeof(float) != 0) return HYDRA_ERR_ALIGN;
+  const size_t n = out->cu.size() - 1;
+  out->pe.assign(out->cu.begin(), out->cu.begin() + int64_t(n));
+  for (size_t d = 0; sc->prefix_len && d < n; ++d) {
+    if (sc->prefix_len[d] < 0 || sc->prefix_len[d] > out->cu[d + 1] - out->cu[d]) return HYDRA_ERR_INVALID;
+    out->pe[d] += sc->prefix_len[d];
+  }
+  out->scored = true;
+  out->softcap = sc->softcap;
+  out->slopes = sc->slopes;
+  return HYDRA_OK;
+}
+
 void plan_items(const Problem& pr, int which, std::vector<int32_t>* items) {
   const hydra_chunk_t& own = which == 0 ? pr.q : pr.kv;
   const hydra_chunk_t& other = which == 0 ? pr.kv : pr.q;
@@ -171,9 +191,13 @@ void plan_items(const Problem& pr, int which, std::vector<int32_t>* items) {
     if (which == 0) {  // keys seen by queries [first, last]
       lo = pr.cu[doc_index(pr.cu, first)];
       hi = last;
+      if (pr.scored) hi = std::max<int64_t>(hi, int64_t(pr.pe[size_t(doc_index(pr.cu, last))]) - 1);
     } else {           // queries that see keys [first, last]
       lo = first;
       hi = int64_t(pr.cu[doc_index(pr.cu, last) + 1]) - 1;
+      // a prefix key is seen from its document's start on; in whole blocks of 32 rows, as the stored dS is
+      // laid out (the rows before the document are masked)
+      if (const size_t d = size_t(doc_index(pr.cu, first)); pr.scored && first < pr.pe[d]) lo = pr.cu[d] & ~31;
     }
     it[3] = ranges_in(other, lo, hi, it + 4);
     for (int r = 0; r < it[3]; ++r) cost[i] += it[4 + 3 * r + 2];
@@ -354,7 +378,10 @@ int64_t visible_pairs(const Problem& pr) {
       int d0 = doc_index(pr.cu, qa), d1 = doc_index(pr.cu, qb - 1);
       for (int d = std::max(d0, 0); d <= d1 && d < n_docs; ++d) {
         const int64_t da = pr.cu[d], db = pr.cu[d + 1];
-        total += causal_pairs(std::max(qa, da), std::min(qb, db), std::max(ka, da), std::min(kb, db));
+        const int64_t q0 = std::max(qa, da), q1 = std::min(qb, db), k0 = std::max(ka, da), k1 = std::min(kb, db);
+        const int64_t pe = pr.scored ? pr.pe[size_t(d)] : da;
+        if (q1 > q0) total += (q1 - q0) * std::max<int64_t>(0, std::min(k1, pe) - k0);
+        total += causal_pairs(q0, q1, std::max(k0, pe), k1);
       }
     }
   }
@@ -424,7 +451,7 @@ WsLayout ws_layout(const Problem& pr, bool noalloc) {
   w.kitems_off = off;
   off = align_up(off + size_t(nkt) * kUnitInts * sizeof(int32_t), 256);
   w.cu_off = off;
-  off = align_up(off + pr.cu.size() * sizeof(int32_t), 256);
+  off = align_up(off + (pr.cu.size() + pr.pe.size()) * sizeof(int32_t), 256);
   w.qitems_off = off;
   off = align_up(off + size_t(nqt) * kUnitInts * sizeof(int32_t), 256);
   w.lists_off = off;
@@ -466,6 +493,7 @@ void plan_image(const Problem& pr, const WsLayout& w, PlanFor call, bool lists, 
     put(w.kitems_off, krecs);
   }
   put(w.cu_off, pr.cu);
+  put(w.cu_off + pr.cu.size() * sizeof(int32_t), pr.pe);
   put(w.qitems_off, qrec);
   if (!lists) return;
   // the split lists last, one after another, so that only what is there is copied

@@ -5,6 +5,7 @@
 #include <vector>
 
 #include "hydra_attn.h"
+#include "hydra_scores.h"
 #include "tiles.h"
 
 namespace hydra {
@@ -25,10 +26,16 @@ struct Problem {
   hydra_chunk_t q{}, kv{};
   int64_t nq = 0, nk = 0;
   int q_s = 0, k_s = 0, v_s = 0;  // token-row strides of q, k, v in elements
+  bool scored = false;         // modified scores (hydra_scores_t); then also
+  float softcap = 0.f;
+  const float* slopes = nullptr;
+  std::vector<int32_t> pe;     // n_docs prefix ends: keys before it are seen by the whole document
 };
 
 // Returns HYDRA_OK or an error status; fills `out` on success.
 int check_problem(const hydra_problem_t* p, Problem* out);
+// The same with modified scores (NULL, or none of them on: the problem without).
+int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out);
 
 // Work items (kItemInts each), heaviest first.  which = 0: query-stationary tiles of
 // kQTile rows with their visible key ranges; which = 1: key-stationary tiles of kKvTile
@@ -78,7 +85,7 @@ void launch_units(const Problem& pr, int which, const std::vector<int32_t>& item
                   const std::vector<int32_t>& kbase, std::vector<int32_t>* units);
 
 // Byte offsets of the workspace regions, in this order: what the stored-dS backward alone reads
-// (krec, qslots), the key items, what the forward reads too (cu, qitems, and at lists the forward's
+// (krec, qslots), the key items, what the forward reads too (cu and with modified scores the prefix ends, qitems, and at lists the forward's
 // split list), the backward's split lists, D and LSE*log2(e).  lists holds the split lists that a plan has, one after
 // another (merges, then units); it has the same size for every problem, so that no problem needs
 // more workspace than one with more rows.  For the no-allocation call, which stores no dS and splits

@@ -41,6 +41,24 @@ class ProblemC(ctypes.Structure):
                 ("v_tok_stride", ctypes.c_int32)]
 
 
+class ScoresC(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float),
+                ("slopes", ctypes.c_void_p),
+                ("prefix_len", ctypes.POINTER(ctypes.c_int32))]
+
+
+ROPE_MAX_AXES = 4
+
+
+class RopeC(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * ROPE_MAX_AXES),
+                ("pairing", ctypes.c_int32),
+                ("per_axis", ctypes.c_int32),
+                ("base", ctypes.c_double),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
 class SchedConfig(ctypes.Structure):
     _fields_ = [("n_ranks", ctypes.c_int32),
                 ("token_budget", ctypes.c_int64),
@@ -151,6 +169,22 @@ def lib() -> ctypes.CDLL:
         L.hydra_unpack_heads_gated.restype = ctypes.c_int
         L.hydra_pack_heads_gated_bwd.argtypes = [i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
         L.hydra_pack_heads_gated_bwd.restype = ctypes.c_int
+        S, sz = ctypes.POINTER(ScoresC), ctypes.c_size_t
+        for name, more, res in (("workspace_size", [], sz), ("scratch_size", [], sz), ("ds_bytes", [i32], sz),
+                                ("visible_pairs", [], i64),
+                                ("plan_items", [i32, ctypes.POINTER(ctypes.c_int32), i64], i64),
+                                ("plan", [vp, sz, vp], ctypes.c_int),
+                                ("fwd", [vp, vp, vp, vp, vp, vp, vp, sz, vp, sz, i32, i32, vp], ctypes.c_int),
+                                ("bwd", [vp] * 9 + [vp, sz, vp, sz, vp, sz, i32, vp], ctypes.c_int)):
+            getattr(L, "hydra_scores_" + name).argtypes = [P, S] + more
+            getattr(L, "hydra_scores_" + name).restype = res
+        R = ctypes.POINTER(RopeC)
+        L.hydra_rope_q.argtypes = [R, i64, i32, i32, i32, vp, i64, vp, vp, vp]
+        L.hydra_rope_kv.argtypes = [R, i64, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.hydra_rope_q_bwd.argtypes = [R, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp]
+        L.hydra_rope_kv_bwd.argtypes = [R, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
+        for name in ("hydra_rope_q", "hydra_rope_kv", "hydra_rope_q_bwd", "hydra_rope_kv_bwd"):
+            getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -167,11 +201,38 @@ def _chunk(segs: Sequence[Tuple[int, int]]) -> Chunk:
     return c
 
 
+class Scores:
+    """How a problem's scores are modified: capped by a tanh (softcap), biased by minus slope times the
+    distance of query and key (slopes: float32 device tensor, one per query head), and a prefix of each
+    document that all of its tokens see (prefix: a length per document).  The cap and the slopes are
+    constants: they get no gradient."""
+
+    def __init__(self, softcap: float = 0.0, slopes=None, prefix: Optional[Sequence[int]] = None):
+        self.softcap, self.slopes = float(softcap), slopes
+        self.prefix = None if prefix is None else np.ascontiguousarray(np.asarray(prefix, dtype=np.int32))
+        self.c = ScoresC()
+        self.c.softcap = self.softcap
+        if slopes is not None:
+            self.c.slopes = _ptr(slopes, "slopes", _F32)
+        if self.prefix is not None:
+            self.c.prefix_len = self.prefix.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+    @property
+    def any(self) -> bool:
+        return self.softcap != 0 or self.slopes is not None or self.prefix is not None
+
+
 class Problem:
-    """One ring step of one rank: head shard, documents, Q chunk and KV chunk."""
+    """One ring step of one rank: head shard, documents, Q chunk and KV chunk; with `scores`, modified
+    scores in every call that takes the problem."""
 
     def __init__(self, cu_seqlens, n_heads: int, q_segs, kv_segs, softmax_scale: float = 0.0,
-                 d_qk: int = 192, d_v: int = 128, n_kv_heads: int = 0):
+                 d_qk: int = 192, d_v: int = 128, n_kv_heads: int = 0, scores: Optional[Scores] = None):
+        if scores is not None and scores.slopes is not None and scores.slopes.numel() != n_heads:
+            raise ValueError(f"slopes: {scores.slopes.numel()} elements, expected {n_heads}")
+        if scores is not None and scores.prefix is not None and scores.prefix.shape != (len(cu_seqlens) - 1,):
+            raise ValueError(f"prefix: shape {scores.prefix.shape}, expected {(len(cu_seqlens) - 1,)}")
+        self.scores = scores
         self.cu = np.ascontiguousarray(np.asarray(cu_seqlens, dtype=np.int32))
         self.q_segs = [tuple(map(int, s)) for s in q_segs]
         self.kv_segs = [tuple(map(int, s)) for s in kv_segs]
@@ -194,14 +255,18 @@ class Problem:
     def ref(self):
         return ctypes.byref(self.c)
 
+    @property
+    def scores_ref(self):
+        return None if self.scores is None else ctypes.byref(self.scores.c)
+
 
 def workspace_size(p: Problem) -> int:
-    return int(lib().hydra_workspace_size(p.ref))
+    return int(lib().hydra_scores_workspace_size(p.ref, p.scores_ref))
 
 
 def split_scratch_size(p: Problem) -> int:
     """Bytes of scratch for the calls' `scratch` (0: nothing of p is split)."""
-    return int(lib().hydra_split_scratch_size(p.ref))
+    return int(lib().hydra_scores_scratch_size(p.ref, p.scores_ref))
 
 
 def noalloc_size(p: Problem) -> int:
@@ -210,18 +275,18 @@ def noalloc_size(p: Problem) -> int:
 
 
 def visible_pairs(p: Problem) -> int:
-    n = int(lib().hydra_visible_pairs(p.ref))
+    n = int(lib().hydra_scores_visible_pairs(p.ref, p.scores_ref))
     if n < 0:
         raise HydraError(-1, "hydra_visible_pairs")
     return n
 
 
 def plan_items(p: Problem, which: int) -> np.ndarray:
-    n = int(lib().hydra_plan_items(p.ref, which, None, 0))
+    n = int(lib().hydra_scores_plan_items(p.ref, p.scores_ref, which, None, 0))
     if n < 0:
         raise HydraError(n, "hydra_plan_items")
     out = np.zeros((max(n, 1), 16), dtype=np.int32)
-    lib().hydra_plan_items(p.ref, which, out.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), n)
+    lib().hydra_scores_plan_items(p.ref, p.scores_ref, which, out.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), n)
     return out[:n]
 
 
@@ -301,8 +366,8 @@ def _set_rows(p: Problem, q, k, v):
 def attn_plan(p: Problem, workspace, stream=None):
     """Uploads the complete work plan of p into workspace (outside any graph capture), for
     the planned calls below."""
-    _check(lib().hydra_attn_plan(p.ref, _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                 _stream(stream)), "hydra_attn_plan")
+    _check(lib().hydra_scores_plan(p.ref, p.scores_ref, _ptr(workspace, "workspace"),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)), "hydra_attn_plan")
 
 
 def _scratch(t) -> Tuple[Optional[int], int]:
@@ -311,11 +376,13 @@ def _scratch(t) -> Tuple[Optional[int], int]:
 
 def _fwd(what: str, merge: bool, p: Problem, q, k, v, o, lse, workspace, o_bf16, stream, planned, scratch):
     nqh = p.nq * p.n_heads
+    if p.scores is not None:
+        _here(p.scores.slopes, q, k, v, o, lse, workspace)
     qp, kp, vp = _set_rows(p, q, k, v)
-    _check(lib().hydra_attn_fwd_split(p.ref, qp, kp, vp, _ptr(o, "o", _F32, nqh * 128), _ptr(lse, "lse", _F32, nqh),
-                                      _ptr(o_bf16, "o_bf16", _BF16, nqh * 128), _ptr(workspace, "workspace"),
-                                      workspace.numel() * workspace.element_size(), *_scratch(scratch), int(merge),
-                                      int(planned), _stream(stream)), what)
+    _check(lib().hydra_scores_fwd(p.ref, p.scores_ref, qp, kp, vp, _ptr(o, "o", _F32, nqh * 128),
+                                  _ptr(lse, "lse", _F32, nqh), _ptr(o_bf16, "o_bf16", _BF16, nqh * 128),
+                                  _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                  *_scratch(scratch), int(merge), int(planned), _stream(stream)), what)
 
 
 def attn_fwd(p: Problem, q, k, v, o_part, lse_part, workspace, o_bf16=None, stream=None, planned=False, scratch=None):
@@ -338,14 +405,16 @@ def attn_fwd_merge(p: Problem, q, k, v, o_acc, lse_acc, workspace, o_bf16=None, 
 def _bwd(what: str, p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, workspace,
          stream, planned, scratch):
     nqh, nkh = p.nq * p.n_heads, p.nk * p.n_kv_heads
+    if p.scores is not None:
+        _here(p.scores.slopes, q, k, v, d_o, dq_acc, dk_acc, dv_acc, workspace)
     qp, kp, vp = _set_rows(p, q, k, v)
-    _check(lib().hydra_attn_bwd_split(p.ref, qp, kp, vp, _ptr(o_final_bf16, "o_final", _BF16, nqh * 128),
-                                      _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
-                                      _ptr(dq_acc, "dq_acc", _F32, nqh * 192), _ptr(dk_acc, "dk_acc", _F32, nkh * 192),
-                                      _ptr(dv_acc, "dv_acc", _F32, nkh * 128), _ptr(ds_buf, "ds_buf"),
-                                      0 if ds_buf is None else ds_buf.numel() * ds_buf.element_size(),
-                                      _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                      *_scratch(scratch), int(planned), _stream(stream)), what)
+    _check(lib().hydra_scores_bwd(p.ref, p.scores_ref, qp, kp, vp, _ptr(o_final_bf16, "o_final", _BF16, nqh * 128),
+                                  _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
+                                  _ptr(dq_acc, "dq_acc", _F32, nqh * 192), _ptr(dk_acc, "dk_acc", _F32, nkh * 192),
+                                  _ptr(dv_acc, "dv_acc", _F32, nkh * 128), _ptr(ds_buf, "ds_buf"),
+                                  0 if ds_buf is None else ds_buf.numel() * ds_buf.element_size(),
+                                  _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                  *_scratch(scratch), int(planned), _stream(stream)), what)
 
 
 def attn_bwd(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, workspace,
@@ -358,7 +427,10 @@ def attn_bwd(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, 
 
 def attn_bwd_noalloc(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, stream=None):
     """attn_bwd with the library's own per-GPU scratch as the workspace (allocates nothing;
-    calls on one GPU must not overlap).  For problems whose noalloc_size is within its 32 MiB."""
+    calls on one GPU must not overlap).  For problems whose noalloc_size is within its 32 MiB, without
+    modified scores."""
+    if p.scores is not None and p.scores.any:
+        raise ValueError("attn_bwd_noalloc has no form for modified scores")
     nqh, nkh = p.nq * p.n_heads, p.nk * p.n_kv_heads
     qp, kp, vp = _set_rows(p, q, k, v)
     _check(lib().hydra_attn_bwd_noalloc(p.ref, qp, kp, vp, _ptr(o_final_bf16, "o_final", _BF16, nqh * 128),
@@ -372,7 +444,7 @@ def attn_bwd_noalloc(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, 
 def bwd_ds_bytes(p: Problem, kv_heads_per_pass: int) -> int:
     """Bytes of dS scratch attn_bwd_ds needs per pass of that many K/V heads (0: the
     stored-dS path does not apply to p)."""
-    return int(lib().hydra_bwd_ds_bytes(p.ref, kv_heads_per_pass))
+    return int(lib().hydra_scores_ds_bytes(p.ref, p.scores_ref, kv_heads_per_pass))
 
 
 def attn_bwd_ds(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, workspace,
@@ -453,6 +525,147 @@ def pack_heads_gated_bwd(y, gate, d_y, d_send, d_gate, stream=None):
            "hydra_pack_heads_gated_bwd")
 
 
+# ------------------------------------------------------------------ rotary positions
+
+class Rope:
+    """Which columns are rotated, in which pairs, by which position and frequency (hydra_rope.h).
+
+    pairs     pairs of each axis (text: one axis; their sum is half the rotated columns)
+    pairing   "interleaved": columns (2j, 2j + 1); "halves": (j, j + half); "axis_halves": halves of each
+              axis' own columns
+    ladder    "whole": frequencies base^(-j / pairs) over all pairs; "axis": anew for each axis
+    inv_freq  instead: every pair's frequency in radians per position
+    """
+    PAIRINGS = ("interleaved", "halves", "axis_halves")
+
+    def __init__(self, pairs: Sequence[int] = (32,), pairing: str = "interleaved", base: float = 10000.0,
+                 ladder: str = "whole", inv_freq: Optional[Sequence[float]] = None):
+        pairs = [int(n) for n in pairs]
+        if not 1 <= len(pairs) <= ROPE_MAX_AXES:
+            raise ValueError(f"1 to {ROPE_MAX_AXES} axes")
+        if pairing not in self.PAIRINGS or ladder not in ("whole", "axis"):
+            raise ValueError(f"unknown pairing {pairing!r} or ladder {ladder!r}")
+        self.n_axes, self.cols = len(pairs), 2 * sum(pairs)
+        self.c = RopeC()
+        self.c.n_axes = len(pairs)
+        for i, n in enumerate(pairs):
+            self.c.pairs[i] = n
+        self.c.pairing = self.PAIRINGS.index(pairing)
+        self.c.per_axis = int(ladder == "axis")
+        self.c.base = base
+        if inv_freq is not None:
+            self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
+            if self.inv_freq.shape != (sum(pairs),):
+                raise ValueError(f"inv_freq: shape {self.inv_freq.shape}, expected {(sum(pairs),)}")
+            self.c.inv_freq = self.inv_freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _here(*tensors):
+    """The launch goes to the current device: every tensor must be there."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != dev:
+            raise ValueError(f"tensor on device {t.device.index}, the current device is {dev}")
+
+
+def _tok_rows(t, what: str, width: int) -> Tuple[int, int]:
+    """Address and token-row stride of bf16 rows of `width` contiguous elements, [T, heads, d] or [T, d]."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: a device tensor is required")
+    if _dt(t) not in _BF16:
+        raise ValueError(f"{what}: dtype {t.dtype} is not one of {_BF16}")
+    if t[0].numel() != width if t.shape[0] else False:
+        raise ValueError(f"{what}: rows of {t[0].numel()} elements, expected {width}")
+    if t.shape[0] and not t[0].is_contiguous():
+        raise ValueError(f"{what}: heads and channels must be contiguous within a token row")
+    if t.shape[0] > 1 and t.stride(0) < width:
+        raise ValueError(f"{what}: token rows {t.stride(0)} elements apart overlap; at least {width} needed")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
+
+
+def _positions(r: Rope, positions, n_tokens: int) -> int:
+    return _ptr(positions, "positions", ("int32",), r.n_axes * n_tokens)
+
+
+def _grad(t, what: str, n: int) -> Tuple[int, int]:
+    if _dt(t) not in _F32 + ("bfloat16",):
+        raise ValueError(f"{what}: dtype {t.dtype} is neither float32 nor bfloat16")
+    return _ptr(t, what, None, n), t.element_size()
+
+
+def rope_q(r: Rope, src, positions, dst, cp_u: int = 1, stream=None):
+    """src [T, H, d] bf16 -> dst [cp_u, T, H/cp_u, d] (cp_u = 1: also [T, H, d]) with the last r.cols columns
+    of every head rotated by positions [n_axes, T] int32.  dst may be src (cp_u = 1): in place."""
+    _here(src, positions, dst)
+    T, H, d = src.shape
+    sp, stride = _tok_rows(src, "src", H * d)
+    if dst.data_ptr() == sp and T:
+        if dst.shape != src.shape or dst.stride() != src.stride():
+            raise ValueError("dst: in place, a tensor of src's shape and strides is required")
+        dp = sp
+    else:
+        dp = _ptr(dst, "dst", _BF16, T * H * d)
+    _check(lib().hydra_rope_q(r.ref, T, H, d, cp_u, sp, stride, _positions(r, positions, T), dp, _stream(stream)),
+           "hydra_rope_q")
+
+
+def rope_q_bwd(r: Rope, dq, positions, d_src, cp_u: int = 1, stream=None):
+    """dq [cp_u, T, H/cp_u, d] float32 (the attention's accumulator) or bf16 -> d_src [T, H, d] bf16, the gradient
+    of rope_q's src."""
+    _here(dq, positions, d_src)
+    T, H, d = d_src.shape
+    gp, gb = _grad(dq, "dq", T * H * d)
+    dp, stride = _tok_rows(d_src, "d_src", H * d)
+    _check(lib().hydra_rope_q_bwd(r.ref, T, H, d, cp_u, gb, gp, _positions(r, positions, T), dp, stride,
+                                  _stream(stream)), "hydra_rope_q_bwd")
+
+
+def _kv_dims(r: Rope, kv, k, v) -> Tuple[int, int, int, int]:
+    T, H, d = kv.shape
+    d_v = 0 if v is None else v.shape[-1]
+    if k.shape[-1] != d - d_v + r.cols:
+        raise ValueError(f"k: heads of {k.shape[-1]} columns, expected {d - d_v + r.cols}")
+    return T, H, d - d_v, d_v
+
+
+def rope_kv(r: Rope, kv, k_pe, positions, k, v=None, cp_u: int = 1, stream=None):
+    """kv [T, H, d_nope + d_v] and the heads' shared k_pe [T, r.cols], bf16 -> k [cp_u, T, H/cp_u, d_nope + r.cols]
+    (a head's keys, then k_pe rotated) and v [cp_u, T, H/cp_u, d_v] (None: kv holds keys only)."""
+    _here(kv, k_pe, positions, k, v)
+    T, H, d_nope, d_v = _kv_dims(r, kv, k, v)
+    sp, stride = _tok_rows(kv, "kv", H * (d_nope + d_v))
+    if k_pe.shape[0] != T:
+        raise ValueError(f"k_pe: {k_pe.shape[0]} rows, expected {T}")
+    pp, pe_stride = _tok_rows(k_pe, "k_pe", r.cols)
+    _check(lib().hydra_rope_kv(r.ref, T, H, d_nope, d_v, cp_u, sp, stride, pp, pe_stride, _positions(r, positions, T),
+                               _ptr(k, "k", _BF16, T * H * (d_nope + r.cols)), _ptr(v, "v", _BF16, T * H * d_v),
+                               _stream(stream)), "hydra_rope_kv")
+
+
+def rope_kv_bwd(r: Rope, dk, dv, positions, d_kv, d_k_pe, cp_u: int = 1, stream=None):
+    """Backward of rope_kv: dk and dv (None: no values), float32 or bf16, as rope_kv's k and v -> d_kv
+    [T, H, d_nope + d_v] and d_k_pe [T, r.cols] (summed over the heads), bf16."""
+    _here(dk, dv, positions, d_kv, d_k_pe)
+    T, H, d_nope, d_v = _kv_dims(r, d_kv, dk, dv)
+    gp, gb = _grad(dk, "dk", T * H * (d_nope + r.cols))
+    vp = None
+    if dv is not None:
+        vp, vb = _grad(dv, "dv", T * H * d_v)
+        if vb != gb:
+            raise ValueError("dk and dv must have one dtype")
+    dp, stride = _tok_rows(d_kv, "d_kv", H * (d_nope + d_v))
+    if d_k_pe.shape[0] != T:
+        raise ValueError(f"d_k_pe: {d_k_pe.shape[0]} rows, expected {T}")
+    pp, pe_stride = _tok_rows(d_k_pe, "d_k_pe", r.cols)
+    _check(lib().hydra_rope_kv_bwd(r.ref, T, H, d_nope, d_v, cp_u, gb, gp, vp, _positions(r, positions, T), dp, stride, pp,
+                                   pe_stride, _stream(stream)), "hydra_rope_kv_bwd")
+
+
 # ------------------------------------------------------------------ scheduler (host only)
 
 def schedule(lengths, n_ranks: int, token_budget: int, pp: int = 1, theta_over_c: float = 0.0, cap: int = 0,
@@ -479,12 +692,12 @@ def profile_start():
 
 def profile_stop() -> dict:
     """Stop timing; returns {kernel: {launches, total_ms, min_ms, max_ms, avg_ms}}."""
-    buf = (KernelStat * 16)()
-    n = lib().hydra_profile_stop(buf, 16)
+    buf = (KernelStat * 32)()
+    n = lib().hydra_profile_stop(buf, 32)
     if n < 0:
         raise HydraError(n, "hydra_profile_stop")
     out = {}
-    for i in range(min(n, 16)):
+    for i in range(min(n, 32)):
         k = buf[i]
         out[k.name.decode()] = dict(launches=k.launches, total_ms=k.total_ms, min_ms=k.min_ms,
                                     max_ms=k.max_ms, avg_ms=k.total_ms / max(k.launches, 1))

@@ -119,8 +119,32 @@ def rank_share(lengths: Sequence[int], mb: Sequence[int], gstart: Sequence[int],
     return RankShare(m, rank, start, k, cp_u, cp_r, u, rho, u * h_rank, h_rank, kv0, n_kv, parts)
 
 
-def problems(share: RankShare, softmax_scale: float = 0.0) -> List[List[hydra.Problem]]:
-    """The hydra problems of every sub-share: one per ring step."""
+def problems(share: RankShare, softmax_scale: float = 0.0, softcap: float = 0.0, slopes=None,
+             prefix: Optional[Sequence[int]] = None) -> List[List[hydra.Problem]]:
+    """The hydra problems of every sub-share: one per ring step; with modified scores as in scores()."""
     nkv = share.n_kv_heads if share.n_kv_heads != share.n_heads else 0
-    return [[hydra.Problem(p.cu, share.n_heads, p.q_segs, st, softmax_scale, n_kv_heads=nkv) for st in p.kv_steps]
-            for p in share.parts]
+    out = []
+    for p in share.parts:
+        sc = scores(share, p, softcap, slopes, prefix)
+        out.append([hydra.Problem(p.cu, share.n_heads, p.q_segs, st, softmax_scale, n_kv_heads=nkv, scores=sc)
+                    for st in p.kv_steps])
+    return out
+
+
+def scores(share: RankShare, part: SubShare, softcap: float = 0.0, slopes=None,
+           prefix: Optional[Sequence[int]] = None) -> Optional[hydra.Scores]:
+    """The modified scores of a sub-share from the model's (slopes: one per query head of the model) and the
+    batch's (prefix: one length per sequence of the batch); None where nothing is modified."""
+    if not softcap and slopes is None and prefix is None:
+        return None
+    return hydra.Scores(softcap, None if slopes is None else slopes[share.head0:share.head0 + share.n_heads].contiguous(),
+                        None if prefix is None else [prefix[i] for i in part.seqs])
+
+
+def doc_positions(part: SubShare, segs: Segs) -> np.ndarray:
+    """Position of every row of `segs` in its own document (int32): what a rotary embedding of packed text
+    takes."""
+    pos = [np.arange(a, a + n) for a, n in segs]
+    pos = np.concatenate(pos) if pos else np.zeros(0, np.int64)
+    cu = np.asarray(part.cu)
+    return (pos - cu[np.searchsorted(cu, pos, side="right") - 1]).astype(np.int32)

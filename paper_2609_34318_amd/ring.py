@@ -59,13 +59,15 @@ def ds_kv_heads_within(probs: Sequence[hydra.Problem], budget_bytes: int) -> int
 
 def make_share(cu_seqlens, n_heads: int, q_segs, kv_steps: Sequence, device="cuda",
                softmax_scale: float = 0.0, n_kv_heads: int = 0, graph_ready: bool = False,
-               ds_kv_heads: int = 0, ds_budget_bytes: int = 0) -> Share:
+               ds_kv_heads: int = 0, ds_budget_bytes: int = 0, scores: Optional[hydra.Scores] = None) -> Share:
     """Plans every ring step of one rank; n_kv_heads (0: n_heads) < n_heads for grouped K/V.
     graph_ready: one workspace per step, for plan() and the planned calls that a graph can
     record.  ds_kv_heads > 0: the backward stores dS instead of recomputing it for dQ, in
     passes of that many K/V heads (a dS scratch sized for the largest step), wherever the
-    stored-dS path applies; or ds_budget_bytes > 0: as many K/V heads per pass as fit it."""
-    probs = [hydra.Problem(cu_seqlens, n_heads, q_segs, s, softmax_scale, n_kv_heads=n_kv_heads) for s in kv_steps]
+    stored-dS path applies; or ds_budget_bytes > 0: as many K/V heads per pass as fit it.  scores:
+    capped, biased or prefix-masked scores, the same in every step."""
+    probs = [hydra.Problem(cu_seqlens, n_heads, q_segs, s, softmax_scale, n_kv_heads=n_kv_heads, scores=scores)
+             for s in kv_steps]
     ws = max(hydra.workspace_size(p) for p in probs)
     if ws == 0:
         raise hydra.HydraError(-1, "hydra_workspace_size")
