@@ -38,7 +38,7 @@ extern "C" {
 /* How the scores are modified.  All fields 0 or NULL, or a NULL hydra_scores_t*: not at all, and
  * the calls below are those of hydra_attn.h, on plans of either. */
 typedef struct {
-  float softcap;              /* c: 0 for none, else from 2^-10 to 2^14                       */
+  float softcap;              /* c: 0 for none, else from 2^-10 to 2^14 and at least softmax_scale / 2^10 */
   const float* slopes;        /* NULL for none, or DEVICE float[n_heads], finite, 4-byte aligned; read when
                                  the kernels run                                               */
   const int32_t* prefix_len;  /* NULL for none, or HOST int32[n_docs], 0 .. the document's
@@ -66,9 +66,11 @@ int hydra_scores_fwd(const hydra_problem_t* p, const hydra_scores_t* sc, const v
                      size_t scratch_bytes, int32_t merge, int32_t planned, void* stream);
 
 /* hydra_attn_bwd_split: dQ, dK and dV of one ring step, added to the accumulators; with ds_buf the
- * stored-dS form where it applies (planned must then be 0). */
+ * stored-dS form where it applies (planned must then be 0).  o_final is bf16 (o_bytes = 2) or the merged
+ * fp32 O itself (4): dQ and dK then do not carry its rounding, which where a few keys take a row's weight
+ * is more than all others together. */
 int hydra_scores_bwd(const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k, const void* v,
-                     const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
+                     const void* o_final, int32_t o_bytes, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
                      float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes,
                      void* scratch, size_t scratch_bytes, int32_t planned, void* stream);
 

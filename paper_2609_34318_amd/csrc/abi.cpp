@@ -17,10 +17,10 @@
 
 namespace hydra {
 hipError_t launch_attn_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
-hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+hipError_t launch_attn_bwd(const AttnArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
                            char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
 hipError_t launch_scores_fwd(const ScoreArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
-hipError_t launch_scores_bwd(const ScoreArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+hipError_t launch_scores_bwd(const ScoreArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
                              char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
 hipError_t launch_lse_merge(int64_t n_rows, int H, float* o_acc, float* lse_acc, const float* o_part,
                             const float* lse_part, uint16_t* o_bf16, hipStream_t stream);
@@ -225,7 +225,16 @@ ScoreArgs score_args(const Problem& pr, const AttnArgs& base) {
   static_cast<AttnArgs&>(a) = base;
   a.pe = base.cu + pr.cu.size();
   a.slopes = pr.slopes;
-  a.cap = pr.softcap;
+  if (pr.softcap > 0.f) {
+    constexpr double log2e = 1.4426950408889634074;
+    const double in = double(pr.scale) / double(pr.softcap), out = double(pr.softcap) * log2e;
+    double x = in * out;
+    for (int k = 0; k < 5; ++k, x *= in * in) a.poly[k] = float(TANH_POLY[k] * x);
+    a.near = float(TANH_NEAR / in);
+    a.two_in = float(2 * log2e * in);
+    a.out = float(out);
+    a.minus_out2 = float(-1 / (out * out));
+  }
   return a;
 }
 
@@ -308,7 +317,7 @@ uint64_t ds_bytes_per_head(const Problem& pr) {
 }
 
 int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k,
-                  const void* v, const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
+                  const void* v, const void* o_final, int o_bytes, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
                   float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, Scratch scratch,
                   void* stream, bool noalloc = false) {
   try {
@@ -338,7 +347,7 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* s
                    vb = rows_bytes(pr.nk, pr.v_s, pr.Hkv * kDv);
     if (outputs_overlap({{dq_acc, qh * kDqk * 4}, {dk_acc, kh * kDqk * 4}, {dv_acc, kh * kDv * 4},
                          {workspace, w.total}, {kv_per_pass ? ds_buf : nullptr, ds_used}, {scratch.at, scratch.bytes}},
-                        {{q, qb}, {k, kb}, {v, vb}, {o_final, qh * kDv * 2}, {lse_final, qh * 4},
+                        {{q, qb}, {k, kb}, {v, vb}, {o_final, qh * kDv * uint64_t(o_bytes)}, {lse_final, qh * 4},
                          {d_o, qh * kDv * 2}, {pr.slopes, uint64_t(pr.H) * 4}}))
       return HYDRA_ERR_INVALID;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -370,8 +379,8 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* s
     const Launch dq = list_launch(workspace, w.qitems_off, w.n_qitems, plan.dq, dq_parts);
     const Launch kv = list_launch(workspace, w.kitems_off, w.n_kitems, plan.kv, kv_parts);
     const hipError_t e =
-        pr.scored ? launch_scores_bwd(score_args(pr, a), q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s)
-                  : launch_attn_bwd(a, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s);
+        pr.scored ? launch_scores_bwd(score_args(pr, a), o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s)
+                  : launch_attn_bwd(a, o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s);
     return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
   } catch (...) {
     return HYDRA_ERR_INVALID;
@@ -412,11 +421,11 @@ int hydra_scores_fwd(const hydra_problem_t* p, const hydra_scores_t* sc, const v
 }
 
 int hydra_scores_bwd(const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k, const void* v,
-                     const void* o_final, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
-                     float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes,
-                     void* scratch, size_t scratch_bytes, int32_t planned, void* stream) {
-  if (planned && ds_buf) return HYDRA_ERR_INVALID;
-  return attn_bwd_impl(planned == 0, p, sc, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+                     const void* o_final, int32_t o_bytes, const float* lse_final, const void* d_o, float* dq_acc,
+                     float* dk_acc, float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace,
+                     size_t workspace_bytes, void* scratch, size_t scratch_bytes, int32_t planned, void* stream) {
+  if ((planned && ds_buf) || (o_bytes != 2 && o_bytes != 4)) return HYDRA_ERR_INVALID;
+  return attn_bwd_impl(planned == 0, p, sc, q, k, v, o_final, o_bytes, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
                        workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 
@@ -447,14 +456,14 @@ int hydra_attn_fwd_split(const hydra_problem_t* p, const void* q, const void* k,
 int hydra_attn_bwd(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
                    const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc, float* dv_acc,
                    void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
+  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
                        workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_bwd_ds(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
                       const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc, float* dv_acc,
                       void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
                        workspace, workspace_bytes, Scratch{}, stream);
 }
 
@@ -512,7 +521,7 @@ int hydra_attn_bwd_noalloc(const hydra_problem_t* p, const void* q, const void* 
     if (noalloc_bytes(pr) > kNoAllocLimitBytes) return HYDRA_ERR_TOO_LARGE;
     void* ws = nullptr;
     if ((rc = scratch_ptr(&ws)) != HYDRA_OK) return rc;
-    return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, ws,
+    return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, ws,
                          kNoAllocScratchBytes, Scratch{}, stream, true);
   } catch (...) {
     return HYDRA_ERR_INVALID;
@@ -537,7 +546,7 @@ size_t hydra_bwd_ds_bytes(const hydra_problem_t* p, int32_t kv_heads_per_pass) {
 int hydra_attn_bwd_planned(const hydra_problem_t* p, const void* q, const void* k, const void* v,
                            const void* o_final, const float* lse_final, const void* d_o, float* dq_acc,
                            float* dk_acc, float* dv_acc, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(false, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
+  return attn_bwd_impl(false, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
                        workspace_bytes, Scratch{}, stream);
 }
 
@@ -546,7 +555,7 @@ int hydra_attn_bwd_split(const hydra_problem_t* p, const void* q, const void* k,
                          void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, void* scratch,
                          size_t scratch_bytes, int32_t planned, void* stream) {
   if (planned && ds_buf) return HYDRA_ERR_INVALID;
-  return attn_bwd_impl(planned == 0, p, nullptr, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
+  return attn_bwd_impl(planned == 0, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
                        workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 

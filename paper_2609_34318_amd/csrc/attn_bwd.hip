@@ -14,7 +14,9 @@
 //
 // MOD: modified scores (hydra_scores.h, scores.h); kPlain is the attention of hydra_attn.h.  A cap multiplies
 // dS by 1 - tanh^2: the dQ workgroups multiply it into dP - D, role A of dK/dV into the P that it
-// hands to role B, which needs no other.
+// hands to role B, which needs no other.  That P is fp16 times 2^15 (P <= 1: what exceeds 2^-29 keeps 11 bits, against
+// the 8 of bf16, so that dS is rounded once to 8 bits, not twice); dS, the stored one too, and dK's
+// accumulator then hold 2^15 times their values, which the last factor takes out.
 #include "kernels.h"
 #include "prof.h"
 #include "scores.h"
@@ -22,7 +24,9 @@
 namespace hydra {
 
 // ------------------------------------------------------------------ D = rowsum(dO * O)
-__global__ __launch_bounds__(256) void bwd_pre_kernel(const uint16_t* __restrict__ o,
+// O_BYTES: of O's elements, bf16 or fp32.
+template <int O_BYTES>
+__global__ __launch_bounds__(256) void bwd_pre_kernel(const void* __restrict__ o,
                                                       const uint16_t* __restrict__ dO,
                                                       const float* __restrict__ lse,
                                                       float* __restrict__ D, float* __restrict__ lse2,
@@ -32,13 +36,25 @@ __global__ __launch_bounds__(256) void bwd_pre_kernel(const uint16_t* __restrict
   // (row, head) pairs, 16 lanes each, strided over a capped grid; the 16 lanes of a pair
   // stay together, so the reduction below always has all of them
   for (int64_t rh = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); rh < total; rh += (int64_t)gridDim.x * 16) {
-    const u32x4 uo = ldg16(o + rh * DV + sub * 8);
+    const char* po = static_cast<const char*>(o) + (rh * DV + sub * 8) * O_BYTES;
+    const u32x4 uo = ldg16(po);
+    u32x4 uo2;
+    if constexpr (O_BYTES == 4) uo2 = ldg16(po + 16);
     const u32x4 ud = ldg16(dO + rh * DV + sub * 8);
     float acc = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      acc += __uint_as_float(uo[w] << 16) * __uint_as_float(ud[w] << 16);
-      acc += __uint_as_float(uo[w] & 0xffff0000u) * __uint_as_float(ud[w] & 0xffff0000u);
+      float o0, o1;
+      if constexpr (O_BYTES == 4) {
+        const u32x4& x = w < 2 ? uo : uo2;
+        o0 = __uint_as_float(x[2 * (w & 1)]);
+        o1 = __uint_as_float(x[2 * (w & 1) + 1]);
+      } else {
+        o0 = __uint_as_float(uo[w] << 16);
+        o1 = __uint_as_float(uo[w] & 0xffff0000u);
+      }
+      acc += o0 * __uint_as_float(ud[w] << 16);
+      acc += o1 * __uint_as_float(ud[w] & 0xffff0000u);
     }
     acc += __shfl_xor(acc, 8, 16);
     acc += __shfl_xor(acc, 4, 16);
@@ -115,15 +131,26 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
-  const ScoreConst sc = score_const<MOD>(a, head);
+  const float slope2 = slope_log2<MOD>(a, head);
   settle(lse2);
   settle(neg_D);
+  // With a cap the kernel needs some 14 registers more than it has: four of Q's fragments then stay in
+  // LDS behind the stages (spilled, their reloads also waited for the tile copies: 16K rows x 8 heads CAP_SPILL)
+  constexpr int Q_LDS = (MOD & kCap) ? 4 : 0, Q_REG = DQK / 16 - Q_LDS;
+  static_assert(DQ_NSTAGE * DQ_STAGE + DQ_WAVES * Q_LDS * 1024 <= DQ_LDS, "LDS");
+  lds_char* q_lds = smem + DQ_NSTAGE * DQ_STAGE + wave * (Q_LDS * 1024);
   bf16x8 qf[DQK / 16], df[DV / 16];
   wait_dma();
   own_rows_read<DQK>(own, lane, qf);
   own_rows_issue<DV>(own, a.dO, q_row0, q_n, a.H * DV, head, lane);
   wait_dma();
   own_rows_read<DV>(own, lane, df);
+  if constexpr (Q_LDS > 0) {
+    barrier_lds();  // every wave has read its rows, which lie there
+#pragma unroll
+    for (int i = 0; i < Q_LDS; ++i)
+      *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>(q_lds + i * 1024 + lane * 16) = qf[Q_REG + i];
+  }
 
   f32x16 acc[DQK / 32];
 #pragma unroll
@@ -154,15 +181,22 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
       constexpr int kb = decltype(kb_)::value;
       f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-      for (int t2 = 0; t2 < DQK / 16; ++t2) s = mfma(op_b128<DQ_BK>(Ks, o, 32 * kb, t2), qf[t2], s);
+      for (int t2 = 0; t2 < Q_REG; ++t2) s = mfma(op_b128<DQ_BK>(Ks, o, 32 * kb, t2), qf[t2], s);
+      if constexpr (Q_LDS > 0) {
+        const lds_char* ql = lds_opaque(q_lds);  // read again for every block, not kept
+        const int lo = lane_now() * 16;
+#pragma unroll
+        for (int t2 = Q_REG; t2 < DQK / 16; ++t2)
+          s = mfma(op_b128<DQ_BK>(Ks, o, 32 * kb, t2), lds_ld16(ql, lo + (t2 - Q_REG) * 1024), s);
+      }
 #pragma unroll
       for (int t2 = 0; t2 < DV / 16; ++t2) dp = mfma(op_b128<DQ_BK>(Vs, o, 32 * kb, t2), df[t2], dp);
 
       float ds[16];
       if constexpr (in_log2<MOD>()) {
         const int ml = lane_now();
-        score16_grad<MOD, -1>(s, sc, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)),
-                              [&](int e, float f) { dp[e] = (dp[e] + neg_D) * f; });
+        score16<MOD, -1, true>(s, a, slope2, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)),
+                         [&](int e, float f) { dp[e] = (dp[e] + neg_D) * f; });
       }
       // exponent of P, and (dP - D) with the cap's factor
       auto arg = [&](int e) { return in_log2<MOD>() ? s[e] - lse2 : __builtin_fmaf(s[e], sl2, -lse2); };
@@ -360,7 +394,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     for (int t = 0; t < n_tiles; ++t) {
       refresh(o);
       const int qpos = cur.q.pos0, qn = cur.q.n;
-      const ScoreConst score_c = score_const<MOD>(a, head0 + cur.member);  // the slope is the query head's
+      const float slope2 = slope_log2<MOD>(a, head0 + cur.member);  // the query head's
       const int64_t ds_off = (int64_t)(ds_head0 + cur.member) * a.ds_head_bytes +
                              (int64_t)(ds_slot0 + cur.qt) * DS_TILE_BYTES;  // this tile's dS slot
       const bool more = t + 1 < n_tiles;
@@ -415,8 +449,8 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             float p[16], f[16];
             if constexpr (in_log2<MOD>()) {
               const int ml = lane_now();
-              score16_grad<MOD, 1>(s, score_c, float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31))),
-                                   [&](int e, float g) { f[e] = g; });
+              score16<MOD, 1, false>(s, a, slope2, float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31))),
+                              [&](int e, float g) { f[e] = g; });
             }
             auto arg = [&](int e) {
               return in_log2<MOD>() ? s[e] - lse_r[e] : __builtin_fmaf(s[e], sl2, -lse_r[e]);
@@ -439,11 +473,11 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             }
             pk[2 * sb] = to_bf16x8(p);
             pk[2 * sb + 1] = to_bf16x8(p + 8);
-            if constexpr (MOD & kCap) {
+            if constexpr (MOD != kPlain) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) p[e] *= f[e];
-              lds_st16<2048 * sb>(pbuf, poff, to_bf16x8(p));
-              lds_st16<2048 * sb + 1024>(pbuf, poff, to_bf16x8(p + 8));
+              for (int e = 0; e < 16; ++e) p[e] *= (MOD & kCap) ? f[e] * P16 : P16;
+              lds_st16<2048 * sb>(pbuf, poff, to_f16x8(p));
+              lds_st16<2048 * sb + 1024>(pbuf, poff, to_f16x8(p + 8));
             } else {
               lds_st16<2048 * sb>(pbuf, poff, pk[2 * sb]);
               lds_st16<2048 * sb + 1024>(pbuf, poff, pk[2 * sb + 1]);
@@ -515,7 +549,8 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             float ds[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float pv = (float)pr[sb][e >> 3][e & 7];
+              const float pv = MOD != kPlain ? (float)__builtin_bit_cast(f16x8, pr[sb][e >> 3])[e & 7]
+                                             : (float)pr[sb][e >> 3][e & 7];
               ds[e] = pv * dp[sb][e];
             }
             sf[sb][0] = to_bf16x8(ds);
@@ -558,7 +593,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     if constexpr (ROLE == 0)
       rows_add<DV / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, 1.0f, a.dv + krow * DV, a.Hkv * DV, kn_w);
     else
-      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, a.scale, a.dk + krow * DQK, a.Hkv * DQK, kn_w);
+      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, ds_scale<MOD>(a.scale), a.dk + krow * DQK, a.Hkv * DQK, kn_w);
   };
   if (role == 0) run(IntC<0>{});
   else run(IntC<1>{});
@@ -790,7 +825,7 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Ar
   }
 
   barrier_lds();  // every wave is past its last tile
-  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, a.scale, a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
+  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, ds_scale<MOD>(a.scale), a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
                      a.H * DQK, wave_rows ? 32 : 0);
 }
 
@@ -859,7 +894,10 @@ hipError_t launch_list(K kernel, const char* name, const A& a, int heads, hipStr
 }
 
 // The merges of n_q split query items and n_kv split key items.
-hipError_t launch_merges(const AttnArgs& q, int n_q, const AttnArgs& kv, int n_kv, hipStream_t stream) {
+template <int MOD>
+hipError_t launch_merges(const AttnArgs& q, int n_q, const AttnArgs& kv_args, int n_kv, hipStream_t stream) {
+  AttnArgs kv = kv_args;
+  kv.scale = ds_scale<MOD>(kv.scale);
   const int q_blocks = n_q * q.q_heads * merge_blocks<true>(), kv_blocks = n_kv * kv.kv_heads * merge_blocks<false>();
   if (q_blocks + kv_blocks == 0) return hipSuccess;
   const int tok = prof_begin("bwd_merge", stream);
@@ -877,7 +915,7 @@ hipError_t launch_recompute(const Args<MOD>& q, int q_merges, const Args<MOD>& k
   hipLaunchKernelGGL(bwd_recompute_kernel<MOD>, dim3(unsigned(kv_blocks + nq)), dim3(512), 0, stream, q, kv);
   prof_end(tok, stream);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return launch_merges(q, q_merges, kv, kv_merges, stream);
+  return launch_merges<MOD>(q, q_merges, kv, kv_merges, stream);
 }
 
 // kv_heads_per_pass = 0: recompute path over all heads.  kv_parts, dq_parts: where the parts of dK/dV
@@ -885,14 +923,14 @@ hipError_t launch_recompute(const Args<MOD>& q, int q_merges, const Args<MOD>& k
 // Otherwise the stored-dS path, in passes of that many K/V heads (the dS of one pass's query heads
 // fits a.ds): bwd_dkdv_ds stores dS, then bwd_dq_ds reads it back.
 template <int MOD>
-hipError_t launch_bwd(const Args<MOD>& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
+hipError_t launch_bwd(const Args<MOD>& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
                       char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
   constexpr bool plain = MOD == kPlain;
   const int64_t pairs = (int64_t)a.nq * a.H;
   const int64_t blocks = (pairs + 15) / 16 < (1 << 20) ? (pairs + 15) / 16 : (1 << 20);
   int tok = prof_begin("bwd_pre", stream);
-  hipLaunchKernelGGL(bwd_pre_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a.o, a.dO, a.lse, a.Dvec,
-                     a.lse2, a.nq, a.H);
+  hipLaunchKernelGGL(o_bytes == 4 ? bwd_pre_kernel<4> : bwd_pre_kernel<2>, dim3((unsigned)blocks), dim3(256), 0,
+                     stream, a.o, a.dO, a.lse, a.Dvec, a.lse2, a.nq, a.H);
   prof_end(tok, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -908,7 +946,7 @@ hipError_t launch_bwd(const Args<MOD>& a, const Launch& q_whole, const Launch& d
       if ((e = launch_list(bwd_dkdv_ds_kernel<MOD>, plain ? "bwd_dkdv_ds" : "bwd_dkdv_ds_scores", b, G, stream)) !=
           hipSuccess)
         return e;
-      if ((e = launch_merges(b, 0, b, kv.n_merges, stream)) != hipSuccess) return e;
+      if ((e = launch_merges<MOD>(b, 0, b, kv.n_merges, stream)) != hipSuccess) return e;
       if ((e = launch_list(bwd_dq_ds_kernel<plain ? kPlain : kScored>, plain ? "bwd_dq_ds" : "bwd_dq_ds_scores",
                            list_args(b, q_whole, nullptr), G * a.grp, stream)) != hipSuccess)
         return e;
@@ -929,15 +967,15 @@ hipError_t launch_bwd(const Args<MOD>& a, const Launch& q_whole, const Launch& d
 
 }  // namespace
 
-hipError_t launch_attn_bwd(const AttnArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                           char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
-  return launch_bwd<kPlain>(a, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
+hipError_t launch_attn_bwd(const AttnArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts,
+                           const Launch& kv, char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+  return launch_bwd<kPlain>(a, o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
 }
 
-hipError_t launch_scores_bwd(const ScoreArgs& a, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                             char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+hipError_t launch_scores_bwd(const ScoreArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts,
+                             const Launch& kv, char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
   return with_mod(a, [&](auto mod) {
-    return launch_bwd<decltype(mod)::value>(a, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
+    return launch_bwd<decltype(mod)::value>(a, o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_heads_per_pass, stream);
   });
 }
 

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
   }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
-  const ScoreConst sc = score_const<MOD>(a, head);
+  const float slope2 = slope_log2<MOD>(a, head);
   bf16x8 qf[DQK / 16];
   wait_dma();
   own_rows_read<DQK>(qbuf, lane, qf);
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
     if constexpr (in_log2<MOD>()) {
       const float d0 = float(q_pos0 + m - kpos - 8 * hh);  // distance of the lane's first key
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) score16<MOD, -1>(s[kb], sc, d0 - 32 * kb);
+      for (int kb = 0; kb < 2; ++kb) score16<MOD, -1, false>(s[kb], a, slope2, d0 - 32 * kb, [](int, float) {});
     }
     // per wave: in a window of short documents most 256-row tiles straddle a boundary, their
     // 32-row waves seldom

@@ -710,8 +710,18 @@ struct AttnArgs {
 struct ScoreArgs : AttnArgs {
   const int* pe;        // prefix end of each document
   const float* slopes;  // [H], or null
-  float cap;            // 0: none
+  // a cap c (out = 0: none), of raw scores s: c log2(e) tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to
+  // |s| = near
+  float poly[5], near;
+  float two_in;         // 2 log2(e) scale / c
+  float out;            // c log2(e)
+  float minus_out2;     // -1 / out^2
 };
+// The polynomial of least relative error of tanh(x) / x in x^2 for |x| <= TANH_NEAR.
+constexpr double TANH_NEAR = 0.75;
+constexpr double TANH_POLY[5] = {0.99999943, -0.333282515, 0.132589832, -0.050056303, 0.0129296325};
+// P goes from role A to role B of the backward with modified scores as fp16 times this.
+constexpr float P16 = 32768.f;
 
 // What a kernel does to its scores: nothing (the plain kernels), or kScored (the prefix mask) with any of
 // the others.

@@ -157,8 +157,9 @@ int check_problem(const hydra_problem_t* p, Problem* out) {
 int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out) {
   const int rc = check_problem(p, out);
   if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len)) return rc;
-  // beyond these the cap's square or the score in units of it leaves the 32-bit range for ordinary inputs
-  if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p14f)) return HYDRA_ERR_INVALID;
+  // the constants of a capped kernel hold powers of softmax_scale / cap up to the ninth
+  if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p14f && out->scale <= 0x1p10f * sc->softcap))
+    return HYDRA_ERR_INVALID;
   if (reinterpret_cast<uintptr_t>(sc->slopes) % sizeof(float) != 0) return HYDRA_ERR_ALIGN;
   const size_t n = out->cu.size() - 1;
   out->pe.assign(out->cu.begin(), out->cu.begin() + int64_t(n));

@@ -44,56 +44,56 @@ __device__ __forceinline__ Span row_span(const int* __restrict__ cu, const int* 
   return {start, max(pos + 1, prefix)};
 }
 
-// What turns raw scores into log2 units, the same for all rows of a head.
-struct ScoreConst {
-  float sl2;     // softmax scale * log2(e)
-  float in;      // softmax scale / cap
-  float out;     // cap * log2(e)
-  float slope2;  // slope * log2(e)
-};
-template <int MOD> __device__ __forceinline__ ScoreConst score_const(const Args<MOD>& a, int head) {
-  ScoreConst c = {a.scale * LOG2E, 0.f, 0.f, 0.f};
-  if constexpr (MOD & kCap) {
-    c.in = a.scale / a.cap;
-    c.out = a.cap * LOG2E;
-  }
-  if constexpr (MOD & kBias) c.slope2 = __int_as_float(((cint*)a.slopes)[head]) * LOG2E;
-  return c;
+// What turns raw scores into log2 units, the same for all rows of a head: the scale, or the cap's constants
+// (ScoreArgs), and the slope * log2(e).
+template <int MOD> __device__ __forceinline__ float slope_log2(const Args<MOD>& a, int head) {
+  if constexpr (MOD & kBias) return __int_as_float(((cint*)a.slopes)[head]) * LOG2E;
+  return 0.f;
 }
 template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0; }
 
-// tanh(x) for |x| <= TANH_NEAR as x P(x^2): the polynomial of least relative error (6e-7) on that range,
-// fitted to tanh.  A cap is some ten times the scores it is for, so that blocks of scores beyond it are
-// few: the wave takes the exponential form, two quarter-rate instructions an element against none, only
-// for those.
-constexpr float TANH_NEAR = 0.75f;
-__device__ __forceinline__ float tanh_near(float x) {
-  const float y = x * x;
-  float r = 0.0129296325f;
-  r = __builtin_fmaf(r, y, -0.050056303f);
-  r = __builtin_fmaf(r, y, 0.132589832f);
-  r = __builtin_fmaf(r, y, -0.333282515f);
-  r = __builtin_fmaf(r, y, 0.999999435f);
-  return x * r;
-}
-// tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy beyond TANH_NEAR; infinite x gives 1
-__device__ __forceinline__ float tanh_any(float x) {
-  const float e = __builtin_amdgcn_exp2f(__builtin_fabsf(x) * (2 * LOG2E));
-  const float far = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f);
-  return __builtin_fabsf(x) > TANH_NEAR ? __builtin_copysignf(far, x) : tanh_near(x);
-}
-
-// 16 raw scores -> tanh(s * in)
-__device__ __forceinline__ void tanh16(f32x16& s, float in) {
+// cap * log2(e) * tanh(s * scale / cap) of 16 raw scores s.  Up to |s| = near (TANH_NEAR caps) it is s times a
+// polynomial in s^2, of least relative error (7e-7): tanh(x) / x = P(x^2), with the caps and the scale in
+// its coefficients.  A cap is some ten times the scores it is for, so blocks that hold a score beyond that
+// are few, and only for them the wave takes the exponential form, two quarter-rate instructions an element:
+// tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.
+// done(e0) follows each group of four elements, whose chains of dependent instructions fill each other's
+// latency.
+template <class D> __device__ __forceinline__ void cap16(f32x16& s, const ScoreArgs& a, D&& done) {
+  // opaque: an instruction reads one scalar register, and the compiler keeps a copy of every second constant
+  // in a vector register through the tile loop
+  float c3 = a.poly[3], out = a.out;
+  asm volatile("" : "+s"(c3), "+s"(out));
   float top = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; e += 2) top = fmax2(fmax2(top, __builtin_fabsf(s[e])), __builtin_fabsf(s[e + 1]));
-  if (__builtin_amdgcn_ballot_w64(top * in > TANH_NEAR) != 0) {
+  const bool far = __builtin_amdgcn_ballot_w64(top > a.near) != 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = tanh_any(s[e] * in);
-  } else {
+  for (int e0 = 0; e0 < 16; e0 += 4) {
+    float w[4], r[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = tanh_near(s[e] * in);
+    for (int i = 0; i < 4; ++i) w[i] = s[e0 + i] * s[e0 + i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(a.poly[4], w[i], c3);
+#pragma unroll
+    for (int k = 2; k >= 0; --k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], a.poly[k]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] *= s[e0 + i];
+    if (far) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = s[e0 + i];
+        const float y = __builtin_amdgcn_exp2f(__builtin_fabsf(x) * a.two_in);
+        float z = __builtin_fmaf(-2.f * out, __builtin_amdgcn_rcpf(y + 1.f), out);
+        settle(z);  // computed for every lane: a branch around it would be taken element by element
+        r[i] = __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
+    done(e0);
   }
 }
 
@@ -102,45 +102,41 @@ template <int DIR> __device__ __forceinline__ float biased(float s, float slope2
   return __builtin_fmaf(-slope2, __builtin_fabsf(d0 + DIR * float(16 * (e >> 3) + (e & 7))), s);
 }
 
-// 16 raw scores -> log2 units.
-template <int MOD, int DIR> __device__ __forceinline__ void score16(f32x16& s, const ScoreConst& c, float d0) {
-  if constexpr (MOD & kCap) {
-    tanh16(s, c.in);
+// 16 raw scores -> log2 units; g(e, 1 - tanh^2) for every element of a capped block.  TIGHT: element groups one
+// after another, for a kernel that has no registers for more.
+template <int MOD, int DIR, bool TIGHT, class G>
+__device__ __forceinline__ void score16(f32x16& s, const Args<MOD>& a, float slope2, float d0, G&& g) {
+  auto rest = [&](int e0) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] *= c.out;
+    for (int e = e0; e < e0 + 4; ++e) {
+      if constexpr (MOD & kCap) g(e, __builtin_fmaf(s[e] * s[e], a.minus_out2, 1.f));
+      else s[e] *= a.scale * LOG2E;
+      if constexpr (MOD & kBias) s[e] = biased<DIR>(s[e], slope2, d0, e);
+    }
+    if constexpr (TIGHT) sched_fence();
+  };
+  if constexpr (MOD & kCap) {
+    cap16(s, a, rest);
   } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] *= c.sl2;
-  }
-  if constexpr (MOD & kBias) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = biased<DIR>(s[e], c.slope2, d0, e);
+    for (int e0 = 0; e0 < 16; e0 += 4) rest(e0);
   }
 }
 
-// The same, and g(e, 1 - tanh^2) for every element of a capped block.
-template <int MOD, int DIR, class G>
-__device__ __forceinline__ void score16_grad(f32x16& s, const ScoreConst& c, float d0, G&& g) {
-  if constexpr (MOD & kCap) {
-    tanh16(s, c.in);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      g(e, __builtin_fmaf(-s[e], s[e], 1.f));
-      s[e] *= c.out;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] *= c.sl2;
-  }
-  if constexpr (MOD & kBias) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = biased<DIR>(s[e], c.slope2, d0, e);
-  }
+// The factor of sums over dS (P16).
+template <int MOD> __host__ __device__ constexpr float ds_scale(float scale) { return MOD == kPlain ? scale : scale / P16; }
+
+// Eight 32-bit values -> fp16, round to nearest even, in the registers of an operand fragment.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bf16x8 to_f16x8(const float* v) {
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  const f32x8 x = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  return __builtin_bit_cast(bf16x8, __builtin_convertvector(x, f16x8));
 }
 
 // f with the variant of a problem's scores as a compile-time number.
 template <class F> hipError_t with_mod(const ScoreArgs& a, F&& f) {
-  if (a.cap > 0.f) return a.slopes ? f(IntC<kScored | kCap | kBias>{}) : f(IntC<kScored | kCap>{});
+  if (a.out > 0.f) return a.slopes ? f(IntC<kScored | kCap | kBias>{}) : f(IntC<kScored | kCap>{});
   return a.slopes ? f(IntC<kScored | kBias>{}) : f(IntC<kScored>{});
 }
 

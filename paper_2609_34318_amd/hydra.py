@@ -175,7 +175,7 @@ def lib() -> ctypes.CDLL:
                                 ("plan_items", [i32, ctypes.POINTER(ctypes.c_int32), i64], i64),
                                 ("plan", [vp, sz, vp], ctypes.c_int),
                                 ("fwd", [vp, vp, vp, vp, vp, vp, vp, sz, vp, sz, i32, i32, vp], ctypes.c_int),
-                                ("bwd", [vp] * 9 + [vp, sz, vp, sz, vp, sz, i32, vp], ctypes.c_int)):
+                                ("bwd", [vp] * 4 + [i32] + [vp] * 5 + [vp, sz, vp, sz, vp, sz, i32, vp], ctypes.c_int)):
             getattr(L, "hydra_scores_" + name).argtypes = [P, S] + more
             getattr(L, "hydra_scores_" + name).restype = res
         R = ctypes.POINTER(RopeC)
@@ -402,14 +402,15 @@ def attn_fwd_merge(p: Problem, q, k, v, o_acc, lse_acc, workspace, o_bf16=None, 
     _fwd("hydra_attn_fwd_merge", True, p, q, k, v, o_acc, lse_acc, workspace, o_bf16, stream, planned, scratch)
 
 
-def _bwd(what: str, p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, workspace,
+def _bwd(what: str, p: Problem, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, workspace,
          stream, planned, scratch):
     nqh, nkh = p.nq * p.n_heads, p.nk * p.n_kv_heads
     if p.scores is not None:
         _here(p.scores.slopes, q, k, v, d_o, dq_acc, dk_acc, dv_acc, workspace)
     qp, kp, vp = _set_rows(p, q, k, v)
-    _check(lib().hydra_scores_bwd(p.ref, p.scores_ref, qp, kp, vp, _ptr(o_final_bf16, "o_final", _BF16, nqh * 128),
-                                  _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
+    _check(lib().hydra_scores_bwd(p.ref, p.scores_ref, qp, kp, vp,
+                                  _ptr(o_final, "o_final", _BF16 + _F32 if p.scores else _BF16, nqh * 128),
+                                  o_final.element_size(), _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
                                   _ptr(dq_acc, "dq_acc", _F32, nqh * 192), _ptr(dk_acc, "dk_acc", _F32, nkh * 192),
                                   _ptr(dv_acc, "dv_acc", _F32, nkh * 128), _ptr(ds_buf, "ds_buf"),
                                   0 if ds_buf is None else ds_buf.numel() * ds_buf.element_size(),
@@ -420,7 +421,8 @@ def _bwd(what: str, p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, d
 def attn_bwd(p: Problem, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, workspace,
              stream=None, planned=False, scratch=None):
     """dQ/dK/dV of one ring step, accumulated (+=) into fp32 buffers (q, k, v, planned and scratch
-    as in attn_fwd)."""
+    as in attn_fwd).  With modified scores o_final may also be the merged fp32 O: dQ and dK then do not
+    carry its rounding to bf16."""
     _bwd("hydra_attn_bwd", p, q, k, v, o_final_bf16, lse_final, d_o, dq_acc, dk_acc, dv_acc, None, workspace, stream,
          planned, scratch)
 

@@ -117,13 +117,18 @@ def forward(sh: Share, q: torch.Tensor, kv: Sequence[Tuple[torch.Tensor, torch.T
     return sh.o_acc, sh.lse_acc, sh.o_bf16
 
 
+def _o_final(sh: Share, p: hydra.Problem) -> torch.Tensor:
+    """What the backward forms D from: with modified scores the unrounded O, which is here anyway."""
+    return sh.o_acc if p.scores is not None else sh.o_bf16
+
+
 def backward(sh: Share, q, kv, d_o, dq: torch.Tensor, dkv: Sequence[Tuple[torch.Tensor, torch.Tensor]],
              planned: bool = False):
     """Accumulates dQ (over steps) and each step's dK/dV; buffers are += targets."""
     for i, (p, (k, v), (dk, dv)) in enumerate(zip(sh.problems, kv, dkv)):
         if sh.ds_buf is not None and not planned:
-            hydra.attn_bwd_ds(p, q, k, v, sh.o_bf16, sh.lse_acc, d_o, dq, dk, dv, sh.ds_buf, sh.workspace,
+            hydra.attn_bwd_ds(p, q, k, v, _o_final(sh, p), sh.lse_acc, d_o, dq, dk, dv, sh.ds_buf, sh.workspace,
                               scratch=sh.scratch)
         else:
-            hydra.attn_bwd(p, q, k, v, sh.o_bf16, sh.lse_acc, d_o, dq, dk, dv, _ws(sh, i, planned),
+            hydra.attn_bwd(p, q, k, v, _o_final(sh, p), sh.lse_acc, d_o, dq, dk, dv, _ws(sh, i, planned),
                            planned=planned, scratch=sh.scratch)
