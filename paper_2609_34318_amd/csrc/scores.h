@@ -52,44 +52,75 @@ template <int MOD> __device__ __forceinline__ float slope_log2(const Args<MOD>& 
 }
 template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0; }
 
-// cap * log2(e) * tanh(s * scale / cap) of 16 raw scores s.  Up to |s| = near (TANH_NEAR caps) it is s times a
+// cap * log2(e) * tanh(s * scale / cap) of raw scores s.  Up to |s| = near (TANH_NEAR caps) it is s times a
 // polynomial in s^2, of least relative error (7e-7): tanh(x) / x = P(x^2), with the caps and the scale in
 // its coefficients.  A cap is some ten times the scores it is for, so blocks that hold a score beyond that
 // are few, and only for them the wave takes the exponential form, two quarter-rate instructions an element:
 // tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.
-// done(e0) follows each group of four elements, whose chains of dependent instructions fill each other's
-// latency.
-template <class D> __device__ __forceinline__ void cap16(f32x16& s, const ScoreArgs& a, D&& done) {
+// Four elements at a time, whose chains of dependent instructions fill each other's latency.
+struct CapConst {
+  float c4, c3, c2, c1, c0, out;
   // opaque: an instruction reads one scalar register, and the compiler keeps a copy of every second constant
   // in a vector register through the tile loop
-  float c3 = a.poly[3], out = a.out;
-  asm volatile("" : "+s"(c3), "+s"(out));
+  __device__ __forceinline__ explicit CapConst(const ScoreArgs& a)
+      : c4(a.poly[4]), c3(a.poly[3]), c2(a.poly[2]), c1(a.poly[1]), c0(a.poly[0]), out(a.out) {
+    asm volatile("" : "+s"(c3), "+s"(out));
+  }
+};
+// Step K of 6 of the polynomial of s[e0 .. e0 + 3], four instructions; r after the last.
+template <int K>
+__device__ __forceinline__ void cap_step(const f32x16& s, int e0, const CapConst& c, float (&w)[4], float (&r)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (K == 0) w[i] = s[e0 + i] * s[e0 + i];
+    if constexpr (K == 1) r[i] = __builtin_fmaf(c.c4, w[i], c.c3);
+    if constexpr (K == 2) r[i] = __builtin_fmaf(r[i], w[i], c.c2);
+    if constexpr (K == 3) r[i] = __builtin_fmaf(r[i], w[i], c.c1);
+    if constexpr (K == 4) r[i] = __builtin_fmaf(r[i], w[i], c.c0);
+    if constexpr (K == 5) r[i] *= s[e0 + i];
+  }
+}
+__device__ __forceinline__ void cap_near4(const f32x16& s, int e0, const CapConst& c, float (&r)[4]) {
+  float w[4];
+  static_for<6>([&](auto k) { cap_step<decltype(k)::value>(s, e0, c, w, r); });
+}
+__device__ __forceinline__ void cap_near16(const f32x16& s, const ScoreArgs& a, f32x16& r) {
+  const CapConst c(a);
+#pragma unroll
+  for (int e0 = 0; e0 < 16; e0 += 4) {
+    float x[4];
+    cap_near4(s, e0, c, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[e0 + i] = x[i];
+  }
+}
+// The exponential form where |x| is beyond near, else r.
+__device__ __forceinline__ float cap_far(float x, float r, const ScoreArgs& a, const CapConst& c) {
+  const float y = __builtin_amdgcn_exp2f(__builtin_fabsf(x) * a.two_in);
+  float z = __builtin_fmaf(-2.f * c.out, __builtin_amdgcn_rcpf(y + 1.f), c.out);
+  settle(z);  // computed for every lane: a branch around it would be taken element by element
+  return __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r;
+}
+__device__ __forceinline__ float cap_top(const f32x16& s) {
   float top = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; e += 2) top = fmax2(fmax2(top, __builtin_fabsf(s[e])), __builtin_fabsf(s[e + 1]));
-  const bool far = __builtin_amdgcn_ballot_w64(top > a.near) != 0;
+  return top;
+}
+__device__ __forceinline__ bool cap_is_far(float top, const ScoreArgs& a) {
+  return __builtin_amdgcn_ballot_w64(top > a.near) != 0;
+}
+// 16 scores in place; done(e0) follows each group.
+template <class D> __device__ __forceinline__ void cap16(f32x16& s, const ScoreArgs& a, D&& done) {
+  const CapConst c(a);
+  const bool far = cap_is_far(cap_top(s), a);
 #pragma unroll
   for (int e0 = 0; e0 < 16; e0 += 4) {
-    float w[4], r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = s[e0 + i] * s[e0 + i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(a.poly[4], w[i], c3);
-#pragma unroll
-    for (int k = 2; k >= 0; --k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], a.poly[k]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] *= s[e0 + i];
+    float r[4];
+    cap_near4(s, e0, c, r);
     if (far) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = s[e0 + i];
-        const float y = __builtin_amdgcn_exp2f(__builtin_fabsf(x) * a.two_in);
-        float z = __builtin_fmaf(-2.f * out, __builtin_amdgcn_rcpf(y + 1.f), out);
-        settle(z);  // computed for every lane: a branch around it would be taken element by element
-        r[i] = __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r[i];
-      }
+      for (int i = 0; i < 4; ++i) r[i] = cap_far(s[e0 + i], r[i], a, c);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
