@@ -426,16 +426,37 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
           for (int t2 = 0; t2 < DQK / 16; ++t2) qa[t2] = op_b128<KV_BQ>(qr_b, 0, t2);
           sched_fence();
           f32x16 sc[KV_NSB];
+          // With a cap, a sub-block's polynomials run under the next one's products, eight instructions after
+          // each, in place; one that holds scores beyond the polynomial's range (few do) is computed
+          // again behind them (16K rows x 8 heads CAP_UNDER)
+          bool far[KV_NSB] = {};
           static_for<KV_NSB>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
             sc[sb] = f32x16{};
-#pragma unroll
-            for (int t2 = 0; t2 < DQK / 16; ++t2) {
+            auto product = [&](int t2) {
               sc[sb] = mfma(qa[t2], bf[t2], sc[sb]);
               if constexpr (sb + 1 < KV_NSB) qa[t2] = op_b128<KV_BQ>(qr_b, 32 * (sb + 1), t2);
+            };
+            if constexpr ((MOD & kCap) && sb > 0) {
+              far[sb - 1] = cap_is_far(cap_top(sc[sb - 1]), a);
+              cap_under<DQK / 16>(sc[sb - 1], a, product);
+            } else {
+#pragma unroll
+              for (int t2 = 0; t2 < DQK / 16; ++t2) product(t2);
             }
             sched_fence();
           });
+          if constexpr (MOD & kCap) {
+            static_for<KV_NSB - 1>([&](auto sb_) {
+              constexpr int sb = decltype(sb_)::value;
+              if (!far[sb]) return;
+              sc[sb] = f32x16{};
+#pragma unroll
+              for (int t2 = 0; t2 < DQK / 16; ++t2) sc[sb] = mfma(op_b128<KV_BQ>(qr_b, 32 * sb, t2), bf[t2], sc[sb]);
+              cap16(sc[sb], a, true, [](int) {});
+            });
+            cap16(sc[KV_NSB - 1], a, cap_is_far(cap_top(sc[KV_NSB - 1]), a), [](int) {});
+          }
           static_for<KV_BQ / 32>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
             const int qb = qpos + 32 * sb;
@@ -447,10 +468,15 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
                                      l2[0], l2[1], l2[2], l2[3], l3[0], l3[1], l3[2], l3[3]};
             const bool full = (kn_w == 32) && (qn >= 32 * (sb + 1)) && (lo_last <= qb) && (qb + 31 < hi_first);
             float p[16], f[16];
-            if constexpr (in_log2<MOD>()) {
+            if constexpr (MOD & kCap) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) f[e] = __builtin_fmaf(s[e] * s[e], a.minus_out2, 1.f);  // 1 - tanh^2
+            }
+            if constexpr (MOD & kBias) {
               const int ml = lane_now();
-              score16<MOD, 1, false>(s, a, slope2, float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31))),
-                              [&](int e, float g) { f[e] = g; });
+              const float d0 = float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31)));
+#pragma unroll
+              for (int e = 0; e < 16; ++e) s[e] = biased<1>((MOD & kCap) ? s[e] : s[e] * sl2, slope2, d0, e);
             }
             auto arg = [&](int e) {
               return in_log2<MOD>() ? s[e] - lse_r[e] : __builtin_fmaf(s[e], sl2, -lse_r[e]);

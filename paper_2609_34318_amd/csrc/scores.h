@@ -58,6 +58,7 @@ template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0
 // are few, and only for them the wave takes the exponential form, two quarter-rate instructions an element:
 // tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.
 // Four elements at a time, whose chains of dependent instructions fill each other's latency.
+// (The functions take any kernel's arguments, so that a plain kernel's discarded branches compile.)
 struct CapConst {
   float c4, c3, c2, c1, c0, out;
   // opaque: an instruction reads one scalar register, and the compiler keeps a copy of every second constant
@@ -84,7 +85,7 @@ __device__ __forceinline__ void cap_near4(const f32x16& s, int e0, const CapCons
   float w[4];
   static_for<6>([&](auto k) { cap_step<decltype(k)::value>(s, e0, c, w, r); });
 }
-__device__ __forceinline__ void cap_near16(const f32x16& s, const ScoreArgs& a, f32x16& r) {
+template <class A> __device__ __forceinline__ void cap_near16(const f32x16& s, const A& a, f32x16& r) {
   const CapConst c(a);
 #pragma unroll
   for (int e0 = 0; e0 < 16; e0 += 4) {
@@ -95,7 +96,7 @@ __device__ __forceinline__ void cap_near16(const f32x16& s, const ScoreArgs& a, 
   }
 }
 // The exponential form where |x| is beyond near, else r.
-__device__ __forceinline__ float cap_far(float x, float r, const ScoreArgs& a, const CapConst& c) {
+template <class A> __device__ __forceinline__ float cap_far(float x, float r, const A& a, const CapConst& c) {
   const float y = __builtin_amdgcn_exp2f(__builtin_fabsf(x) * a.two_in);
   float z = __builtin_fmaf(-2.f * c.out, __builtin_amdgcn_rcpf(y + 1.f), c.out);
   settle(z);  // computed for every lane: a branch around it would be taken element by element
@@ -107,13 +108,12 @@ __device__ __forceinline__ float cap_top(const f32x16& s) {
   for (int e = 0; e < 16; e += 2) top = fmax2(fmax2(top, __builtin_fabsf(s[e])), __builtin_fabsf(s[e + 1]));
   return top;
 }
-__device__ __forceinline__ bool cap_is_far(float top, const ScoreArgs& a) {
+template <class A> __device__ __forceinline__ bool cap_is_far(float top, const A& a) {
   return __builtin_amdgcn_ballot_w64(top > a.near) != 0;
 }
-// 16 scores in place; done(e0) follows each group.
-template <class D> __device__ __forceinline__ void cap16(f32x16& s, const ScoreArgs& a, D&& done) {
+// 16 scores in place (far: cap_is_far of them, or true); done(e0) follows each group.
+template <class A, class D> __device__ __forceinline__ void cap16(f32x16& s, const A& a, bool far, D&& done) {
   const CapConst c(a);
-  const bool far = cap_is_far(cap_top(s), a);
 #pragma unroll
   for (int e0 = 0; e0 < 16; e0 += 4) {
     float r[4];
@@ -126,6 +126,27 @@ template <class D> __device__ __forceinline__ void cap16(f32x16& s, const ScoreA
     for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
     done(e0);
   }
+}
+// 16 near scores in place, by the polynomial, under N = 12 products: product(i) starts the i-th, and eight
+// instructions (32 cycles) follow each.  The fences keep the compiler from moving them behind all products.
+template <int N, class A, class P> __device__ __forceinline__ void cap_under(f32x16& s, const A& a, P&& product) {
+  static_assert(N == 12, "four groups of six steps");
+  const CapConst c(a);
+  float w[4], r[4];
+  static_for<N>([&](auto i_) {
+    constexpr int i = decltype(i_)::value;
+    product(i);
+    cap_step<2 * (i % 3)>(s, 4 * (i / 3), c, w, r);
+    cap_step<2 * (i % 3) + 1>(s, 4 * (i / 3), c, w, r);
+    if constexpr (i % 3 == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        settle(r[e]);  // here, not where it is first used
+        s[4 * (i / 3) + e] = r[e];
+      }
+    }
+    sched_fence();
+  });
 }
 
 // The bias of an element: its distance is |d0 + DIR * (its offset)|.
@@ -147,7 +168,7 @@ __device__ __forceinline__ void score16(f32x16& s, const Args<MOD>& a, float slo
     if constexpr (TIGHT) sched_fence();
   };
   if constexpr (MOD & kCap) {
-    cap16(s, a, rest);
+    cap16(s, a, cap_is_far(cap_top(s), a), rest);
   } else {
 #pragma unroll
     for (int e0 = 0; e0 < 16; e0 += 4) rest(e0);
