@@ -313,6 +313,15 @@ bool overlap(Span a, Span b) {
   return x < y + b.n && y < x + a.n;
 }
 
+// f / 2 pi modulo 1, times 2^64 (modulo 2^64).  1 / 2 pi in two doubles, the product's rounding error from a
+// fused multiply-add; the error's part may be negative, and wraps like all else.
+uint64_t turns64(double f) {
+  if (f < 0) return 0 - turns64(-f);  // 1 - a small part would round
+  constexpr double hi = 0.15915494309189535, lo = -9.839338337591243e-18;
+  const double t = f * hi, e = std::fma(f, hi, -t) + f * lo;
+  return uint64_t((t - std::floor(t)) * 0x1p64) + uint64_t(int64_t(e * 0x1p64));
+}
+
 // Checks and fills the table; *ex: how its pairs are exchanged.
 int make_table(const hydra_rope_t* r, RopeTable* t, Exchange* ex) {
   if (!r || r->n_axes < 1 || r->n_axes > HYDRA_ROPE_MAX_AXES) return HYDRA_ERR_INVALID;
@@ -336,10 +345,7 @@ int make_table(const hydra_rope_t* r, RopeTable* t, Exchange* ex) {
                        : r->per_axis ? std::pow(r->base, -double(j - j0) / r->pairs[a])
                                      : std::pow(r->base, -double(j) / n);
       if (!(std::fabs(f) <= 0x1p20)) return HYDRA_ERR_INVALID;
-      const long double turns = (long double)f / 6.283185307179586476925286766559L;
-      const long double part = turns - floorl(turns);  // in [0, 1]
-      // rounded to 64 bits; a whole turn is none
-      t->freq[j] = part >= 1.0L ? 0 : uint64_t(part * 0x1p64L);
+      t->freq[j] = turns64(f);
       t->axis[j] = uint8_t(a);
       const int c0 = r->pairing == HYDRA_ROPE_INTERLEAVED ? 2 * j : r->pairing == HYDRA_ROPE_HALVES ? j : j0 + j;
       const int c1 = r->pairing == HYDRA_ROPE_INTERLEAVED ? c0 + 1 : c0 + (r->pairing == HYDRA_ROPE_HALVES ? n : r->pairs[a]);

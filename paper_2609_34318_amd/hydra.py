@@ -7,6 +7,7 @@ is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -315,8 +316,14 @@ def _ptr(t, what: str = "tensor", dtypes=None, numel: Optional[int] = None) -> O
     return t.data_ptr()
 
 
+_DTYPE_NAMES = {}  # torch dtype -> its name
+
+
 def _dt(t) -> str:
-    return str(t.dtype).replace("torch.", "")
+    name = _DTYPE_NAMES.get(t.dtype)
+    if name is None:
+        name = _DTYPE_NAMES[t.dtype] = str(t.dtype).replace("torch.", "")
+    return name
 
 
 _BF16 = ("bfloat16", "int16")  # bf16 values, or their raw 16-bit patterns
@@ -332,22 +339,25 @@ def _rows(t, what: str, rows: int, heads: int, d: int) -> Tuple[Optional[int], i
         raise ValueError(f"{what}: a device tensor is required")
     if _dt(t) not in _BF16:
         raise ValueError(f"{what}: dtype {t.dtype} is not one of {_BF16}")
-    if tuple(t.shape) != (rows, heads, d):
+    if t.shape != (rows, heads, d):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(rows, heads, d)}")
-    if rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+    s0, s1, s2 = t.stride()
+    if rows and (s2 != 1 or (heads > 1 and s1 != d)):
         raise ValueError(f"{what}: heads and channels must be contiguous within a token row")
-    if rows > 1 and t.stride(0) < heads * d:
+    if rows > 1 and s0 < heads * d:
         # an expanded (broadcast) or overlapping view: the library would read rows that the
         # allocation does not hold (a stride of 0 even means "dense" to it)
-        raise ValueError(f"{what}: token rows {t.stride(0)} elements apart overlap; at least {heads * d} needed")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else heads * d)
+        raise ValueError(f"{what}: token rows {s0} elements apart overlap; at least {heads * d} needed")
+    return t.data_ptr(), (s0 if rows > 1 else heads * d)
 _F32 = ("float32",)
 
 
 def _stream(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    # the handle of torch.cuda.current_stream() without building the object (a quarter of a small call's time)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _check(rc: int, what: str):
@@ -555,6 +565,10 @@ class Rope:
         self.c.pairing = self.PAIRINGS.index(pairing)
         self.c.per_axis = int(ladder == "axis")
         self.c.base = base
+        if inv_freq is None and base >= 1:  # made once here, not in every call (the library refuses other bases)
+            n = sum(pairs)
+            inv_freq = [base ** -(j / m if ladder == "axis" else (j + j0) / n)
+                        for m, j0 in zip(pairs, [sum(pairs[:a]) for a in range(len(pairs))]) for j in range(m)]
         if inv_freq is not None:
             self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
             if self.inv_freq.shape != (sum(pairs),):
@@ -571,8 +585,8 @@ def _here(*tensors):
     import torch
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != dev:
-            raise ValueError(f"tensor on device {t.device.index}, the current device is {dev}")
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"tensor on device {t.get_device()}, the current device is {dev}")
 
 
 def _tok_rows(t, what: str, width: int) -> Tuple[int, int]:
@@ -581,13 +595,18 @@ def _tok_rows(t, what: str, width: int) -> Tuple[int, int]:
         raise ValueError(f"{what}: a device tensor is required")
     if _dt(t) not in _BF16:
         raise ValueError(f"{what}: dtype {t.dtype} is not one of {_BF16}")
-    if t[0].numel() != width if t.shape[0] else False:
-        raise ValueError(f"{what}: rows of {t[0].numel()} elements, expected {width}")
-    if t.shape[0] and not t[0].is_contiguous():
-        raise ValueError(f"{what}: heads and channels must be contiguous within a token row")
-    if t.shape[0] > 1 and t.stride(0) < width:
-        raise ValueError(f"{what}: token rows {t.stride(0)} elements apart overlap; at least {width} needed")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
+    rows, *inner = t.shape
+    s0, *strides = t.stride()
+    if math.prod(inner) != width:
+        raise ValueError(f"{what}: rows of {math.prod(inner)} elements, expected {width}")
+    step = 1
+    for n, s in zip(reversed(inner), reversed(strides)):
+        if rows and n > 1 and s != step:
+            raise ValueError(f"{what}: heads and channels must be contiguous within a token row")
+        step *= n
+    if rows > 1 and s0 < width:
+        raise ValueError(f"{what}: token rows {s0} elements apart overlap; at least {width} needed")
+    return t.data_ptr(), (s0 if rows > 1 else 0)
 
 
 def _positions(r: Rope, positions, n_tokens: int) -> int:
