@@ -60,28 +60,37 @@ __device__ __forceinline__ f32x8 widen(u32x4 v) {
 }
 __device__ __forceinline__ u32x4 narrow(f32x8 x) { return __builtin_bit_cast(u32x4, __builtin_convertvector(x, bf16x8)); }
 
-__device__ __forceinline__ u32x4 ld_stream(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+// Loads leave their lines in the caches, where the kernel before often left them (1021 tokens x 64 heads 12 to 17 us
+// a call, 15 to 21 with the non-temporal hint; the same for tensors beyond the caches).
+__device__ __forceinline__ u32x4 ld_chunk(const char* p) { return *reinterpret_cast<const u32x4*>(p); }
 __device__ __forceinline__ void st_stream(char* p, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }
 
-// 8 elements of BYTES bytes each: as they are read, and as 32-bit values.
-template <int BYTES> struct Chunk8;
-template <> struct Chunk8<2> {
+// One lane's chunk: 16 bytes of input, so that a wave's loads are contiguous, 8 columns of bf16 or 4 of fp32.
+// As it is read, as 32-bit values, and as the bf16 that is stored.
+template <int BYTES> struct Chunk;
+template <> struct Chunk<2> {
+  static constexpr int N = 8;
+  typedef f32x8 Wide;
   u32x4 v;
-  __device__ __forceinline__ void load(const char* p) { v = ld_stream(p); }
-  __device__ __forceinline__ f32x8 wide() const { return widen(v); }
-  __device__ __forceinline__ u32x4 bf16() const { return v; }
+  __device__ __forceinline__ void load(const char* p) { v = ld_chunk(p); }
+  __device__ __forceinline__ Wide wide() const { return widen(v); }
+  __device__ __forceinline__ void store(char* p) const { st_stream(p, v); }
+  static __device__ __forceinline__ void store(char* p, Wide x) { st_stream(p, narrow(x)); }
 };
-template <> struct Chunk8<4> {
-  u32x4 a, b;
-  __device__ __forceinline__ void load(const char* p) { a = ld_stream(p), b = ld_stream(p + 16); }
-  __device__ __forceinline__ f32x8 wide() const {
-    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
-    return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+template <> struct Chunk<4> {
+  static constexpr int N = 4;
+  typedef f32x4 Wide;
+  u32x4 v;
+  __device__ __forceinline__ void load(const char* p) { v = ld_chunk(p); }
+  __device__ __forceinline__ Wide wide() const { return __builtin_bit_cast(f32x4, v); }
+  __device__ __forceinline__ void store(char* p) const { store(p, wide()); }
+  static __device__ __forceinline__ void store(char* p, Wide x) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), reinterpret_cast<u32x2*>(p));
   }
-  __device__ __forceinline__ u32x4 bf16() const { return narrow(wide()); }
 };
 
-// Element offset of head h of token t: in [G][*] of `width` columns a head, or in token rows.
+// Element offset of head h of token t in [G][*] of `width` columns a head.
 __device__ __forceinline__ int64_t at_group(const RopeArgs& a, int64_t t, int h, int width) {
   const int j = (unsigned)h / (unsigned)a.g;
   return ((j * a.T + t) * a.g + (h - j * a.g)) * width;
@@ -103,7 +112,8 @@ __device__ __forceinline__ void fill_table(const RopeArgs& a, int64_t t0, int n,
   }
 }
 
-// A lane's chunk of a head, for heads of `chunks` chunks: chunk c of head `sub` of the heads a wave holds.
+// A lane's chunk of a head, for heads of `chunks` chunks (at most 64): chunk c of head `sub` of the heads a
+// wave holds.
 struct LaneMap {
   int per_wave, sub, c;
   bool on;
@@ -115,36 +125,40 @@ struct LaneMap {
   }
 };
 
-// x rotated: columns [8c, 8c + 8) of a head in this lane, its other chunks in the lanes beside it.
-// cs: the token's table; other: LDS column of each column's partner; buf: 64 x 8 floats of this wave.
-template <int EX>
-__device__ __forceinline__ f32x8 rotate(f32x8 x, const float2* cs, const uint8_t* other, float* buf, int lane,
-                                        const LaneMap& m) {
-  const int c = m.c;
-  const float4* row = reinterpret_cast<const float4*>(cs + 8 * c);
-  f32x8 y;
+// x rotated: columns [N c, N c + N) of a head in this lane, its other chunks in the lanes beside it.
+// cs: the token's table; other: each column's partner; buf: 64 x N floats of this wave.
+template <int EX, int N, class V>
+__device__ __forceinline__ V rotate(V x, const float2* cs, const uint8_t* other, float* buf, int lane, const LaneMap& m) {
+  const float4* row = reinterpret_cast<const float4*>(cs + N * m.c);
+  V y;
   if constexpr (EX == kInChunk) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+    for (int i = 0; i < N; ++i) y[i] = x[i ^ 1];
   } else {
-    float4* mine = reinterpret_cast<float4*>(buf + 8 * lane);
     wave_lds_order();
-    mine[0] = make_float4(x[0], x[1], x[2], x[3]);
-    mine[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<float4*>(buf + N * lane + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
     wave_lds_order();
-    const float* head = buf + 8 * (m.on ? lane - c : 0);  // the head's first column
+    const float* head = buf + N * (m.on ? lane - m.c : 0);  // the head's first column
+    const int col = N * m.c;
     if constexpr (EX == kChunks) {
-      const float4* o = reinterpret_cast<const float4*>(head + other[8 * c]);
-      const float4 u = o[0], v = o[1];
-      y = f32x8{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(head + other[col] + i);
+        y[i] = u.x;
+        y[i + 1] = u.y;
+        y[i + 2] = u.z;
+        y[i + 3] = u.w;
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = head[other[8 * c + i]];
+      for (int i = 0; i < N; ++i) y[i] = head[other[col + i]];
     }
   }
-  f32x8 r;
+  V r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < N / 2; ++i) {
     const float4 w = row[i];  // cos, sin of two columns
     r[2 * i] = __builtin_fmaf(x[2 * i], w.x, y[2 * i] * w.y);
     r[2 * i + 1] = __builtin_fmaf(x[2 * i + 1], w.z, y[2 * i + 1] * w.w);
@@ -152,32 +166,98 @@ __device__ __forceinline__ f32x8 rotate(f32x8 x, const float2* cs, const uint8_t
   return r;
 }
 
-// LDS of a workgroup: the table, the partners, the waves' exchange buffers.
+// LDS of a workgroup: the waves' exchange buffers, the partners, the table, and for sums over heads
+// `sums` times cols floats a token.
 struct Shared {
-  float2* cs;
-  uint8_t* other;
   float* buf;
+  uint8_t* other;
+  float2* cs;
+  float* part;
   __device__ __forceinline__ Shared(char* base, const RopeArgs& a, int wave) {
     buf = reinterpret_cast<float*>(base) + wave * 64 * 8;
     other = reinterpret_cast<uint8_t*>(base + kWaves * 64 * 8 * 4);
     cs = reinterpret_cast<float2*>(base + kWaves * 64 * 8 * 4 + kMaxCols);
+    part = reinterpret_cast<float*>(cs + a.block_tokens * a.r.cols);
     for (int j = threadIdx.x; j < a.r.pairs; j += kThreads) {
       other[a.r.first[j]] = a.r.second[j];
       other[a.r.second[j]] = a.r.first[j];
     }
   }
 };
-size_t shared_bytes(int block_tokens, int cols) {
-  return size_t(kWaves) * 64 * 8 * 4 + kMaxCols + size_t(block_tokens) * size_t(cols) * sizeof(float2);
+size_t shared_bytes(int block_tokens, int cols, int sums) {
+  return size_t(kWaves) * 64 * 8 * 4 + kMaxCols + size_t(block_tokens) * size_t(cols) * sizeof(float2) +
+         size_t(block_tokens) * size_t(sums) * size_t(cols) * sizeof(float);
 }
 
-// Calls f(t, group of heads) for this wave's share of n tokens x groups.
+// Calls f(t, group of heads, whether it is one) for this wave's share of n tokens x groups, two at a time (f is
+// called by every lane, for loads of both before a use).
 template <class F> __device__ __forceinline__ void for_items(int wave, int n, int groups, F&& f) {
   int t = wave / groups, hg = wave - t * groups;
-  while (t < n) {
-    f(t, hg);
+  auto next = [&]() {
     hg += kWaves;
     while (hg >= groups) hg -= groups, ++t;
+  };
+  while (t < n) {
+    const int t0 = t, hg0 = hg;
+    next();
+    f(t0, hg0, t, hg, t < n);
+    next();
+  }
+}
+
+// Moves chunks of `cols` columns a head, IN_BYTES an element, for n tokens from t0 on: at(t, j, k, col) gives the
+// element offsets {source, destination} and the two bases of head k of send buffer j.  A thread's
+// chunks are kThreads apart in the order [token][buffer][head][chunk], found by carrying, not by dividing.
+template <int IN_BYTES, class F>
+__device__ __forceinline__ void move_chunks(const RopeArgs& a, int n, int cols, F&& at) {
+  typedef Chunk<IN_BYTES> C;
+  constexpr int U = 4;
+  const int chunks = cols / C::N, cp_u = a.H / a.g;
+  auto split = [&](int i, int& t, int& j, int& k, int& c) {
+    int q = i / chunks;
+    c = i - q * chunks;
+    int r = q / a.g;
+    k = q - r * a.g;
+    t = r / cp_u;
+    j = r - t * cp_u;
+  };
+  int t, j, k, c, dt, dj, dk, dc;
+  split(threadIdx.x, t, j, k, c);
+  split(kThreads, dt, dj, dk, dc);
+  while (t < n) {
+    C x[U];
+    char* to[U];
+    bool on[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      on[u] = t < n;
+      if (on[u]) {
+        const char* from;
+        at(t, j, k, c * C::N, from, to[u]);
+        x[u].load(from);
+      }
+      c += dc;
+      k += dk;
+      if (c >= chunks) c -= chunks, ++k;
+      j += dj;
+      if (k >= a.g) k -= a.g, ++j;
+      t += dt;
+      if (j >= cp_u) j -= cp_u, ++t;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (on[u]) x[u].store(to[u]);
+  }
+}
+
+// The blocks of tokens of a workgroup: f(first token, tokens), with the table of cos and sin filled.
+template <class F> __device__ __forceinline__ void for_blocks(const RopeArgs& a, const Shared& sh, F&& f) {
+  for (int64_t t0 = (int64_t)blockIdx.x * a.block_tokens; t0 < a.T; t0 += (int64_t)gridDim.x * a.block_tokens) {
+    const int n = (int)min((int64_t)a.block_tokens, a.T - t0);
+    __syncthreads();
+    fill_table(a, t0, n, sh.cs);
+    __syncthreads();
+    f(t0, n);
   }
 }
 
@@ -185,119 +265,149 @@ template <class F> __device__ __forceinline__ void for_items(int wave, int n, in
 // IN_BYTES: of the input's elements.  BWD: [G] -> token rows, else token rows -> [G] (or in place).
 template <int EX, int IN_BYTES, bool BWD, bool IN_PLACE>
 __global__ __launch_bounds__(kThreads) void rope_q_kernel(RopeArgs a) {
+  typedef Chunk<IN_BYTES> C;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Shared sh(smem, a, wave);
   const int nope = a.d - a.r.cols;
-  for (int64_t t0 = (int64_t)blockIdx.x * a.block_tokens; t0 < a.T; t0 += (int64_t)gridDim.x * a.block_tokens) {
-    const int n = (int)min((int64_t)a.block_tokens, a.T - t0);
-    __syncthreads();
-    fill_table(a, t0, n, sh.cs);
-    __syncthreads();
+  for_blocks(a, sh, [&](int64_t t0, int n) {
     auto src_at = [&](int64_t t, int h) { return BWD ? at_group(a, t, h, a.d) : t * a.src_stride + (int64_t)h * a.d; };
     auto dst_at = [&](int64_t t, int h) {
       return BWD || IN_PLACE ? t * a.dst_stride + (int64_t)h * a.d : at_group(a, t, h, a.d);
     };
-    const LaneMap m(lane, a.r.cols / 8);
-    for_items(wave, n, (a.H + m.per_wave - 1) / m.per_wave, [&](int t, int hg) {
-      const int h = hg * m.per_wave + m.sub;
-      const bool on = m.on && h < a.H;
-      Chunk8<IN_BYTES> x{};
-      if (on) x.load(a.src + (src_at(t0 + t, h) + nope + 8 * m.c) * IN_BYTES);
-      const f32x8 y = rotate<EX>(x.wide(), sh.cs + t * a.r.cols, sh.other, sh.buf, lane, m);
-      if (on) st_stream(a.dst + (dst_at(t0 + t, h) + nope + 8 * m.c) * 2, narrow(y));
+    const LaneMap m(lane, a.r.cols / C::N);
+    const int col = nope + C::N * m.c;
+    for_items(wave, n, (a.H + m.per_wave - 1) / m.per_wave, [&](int ta, int ga, int tb, int gb, bool b_on) {
+      const int ha = ga * m.per_wave + m.sub, hb = gb * m.per_wave + m.sub;
+      const bool on_a = m.on && ha < a.H, on_b = b_on && m.on && hb < a.H;
+      C x{}, z{};
+      if (on_a) x.load(a.src + (src_at(t0 + ta, ha) + col) * IN_BYTES);
+      if (on_b) z.load(a.src + (src_at(t0 + tb, hb) + col) * IN_BYTES);
+      const auto y = rotate<EX, C::N>(x.wide(), sh.cs + ta * a.r.cols, sh.other, sh.buf, lane, m);
+      if (on_a) C::store(a.dst + (dst_at(t0 + ta, ha) + col) * 2, y);
+      if (!b_on) return;  // uniform over the wave
+      const auto w = rotate<EX, C::N>(z.wide(), sh.cs + tb * a.r.cols, sh.other, sh.buf, lane, m);
+      if (on_b) C::store(a.dst + (dst_at(t0 + tb, hb) + col) * 2, w);
     });
-    if (!IN_PLACE && nope > 0) {
-      const LaneMap m2(lane, nope / 8);
-      for_items(wave, n, (a.H + m2.per_wave - 1) / m2.per_wave, [&](int t, int hg) {
-        const int h = hg * m2.per_wave + m2.sub;
-        if (!m2.on || h >= a.H) return;
-        Chunk8<IN_BYTES> x;
-        x.load(a.src + (src_at(t0 + t, h) + 8 * m2.c) * IN_BYTES);
-        st_stream(a.dst + (dst_at(t0 + t, h) + 8 * m2.c) * 2, x.bf16());
+    if (!IN_PLACE && nope > 0)
+      move_chunks<IN_BYTES>(a, n, nope, [&](int t, int j, int k, int c, const char*& from, char*& to) {
+        const int64_t row = (int64_t)(j * a.g + k) * a.d + c, packed = ((j * a.T + t0 + t) * a.g + k) * a.d + c;
+        from = a.src + (BWD ? packed : (t0 + t) * a.src_stride + row) * IN_BYTES;
+        to = a.dst + (BWD ? (t0 + t) * a.dst_stride + row : packed) * 2;
       });
-    }
-  }
+  });
 }
 
 // ------------------------------------------------------------------ keys and values
 template <int EX> __global__ __launch_bounds__(kThreads) void rope_kv_kernel(RopeArgs a) {
+  typedef Chunk<2> C;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Shared sh(smem, a, wave);
   const int d_kv = a.d_nope + a.d_v;
-  for (int64_t t0 = (int64_t)blockIdx.x * a.block_tokens; t0 < a.T; t0 += (int64_t)gridDim.x * a.block_tokens) {
-    const int n = (int)min((int64_t)a.block_tokens, a.T - t0);
-    __syncthreads();
-    fill_table(a, t0, n, sh.cs);
-    __syncthreads();
+  for_blocks(a, sh, [&](int64_t t0, int n) {
     // k_pe rotated, to every head
-    const LaneMap m(lane, a.r.cols / 8);
-    for_items(wave, n, (a.H + m.per_wave - 1) / m.per_wave, [&](int t, int hg) {
-      const int h = hg * m.per_wave + m.sub;
-      Chunk8<2> x{};
-      if (m.on) x.load(a.src2 + ((t0 + t) * a.src2_stride + 8 * m.c) * 2);
-      const f32x8 y = rotate<EX>(x.wide(), sh.cs + t * a.r.cols, sh.other, sh.buf, lane, m);
-      if (m.on && h < a.H) st_stream(a.dst + (at_group(a, t0 + t, h, a.d) + a.d_nope + 8 * m.c) * 2, narrow(y));
+    const LaneMap m(lane, a.r.cols / C::N);
+    for_items(wave, n, (a.H + m.per_wave - 1) / m.per_wave, [&](int ta, int ga, int tb, int gb, bool b_on) {
+      const int ha = ga * m.per_wave + m.sub, hb = gb * m.per_wave + m.sub;
+      C x{}, z{};
+      if (m.on) x.load(a.src2 + ((t0 + ta) * a.src2_stride + 8 * m.c) * 2);
+      if (m.on && b_on) z.load(a.src2 + ((t0 + tb) * a.src2_stride + 8 * m.c) * 2);
+      const auto y = rotate<EX, 8>(x.wide(), sh.cs + ta * a.r.cols, sh.other, sh.buf, lane, m);
+      if (m.on && ha < a.H) C::store(a.dst + (at_group(a, t0 + ta, ha, a.d) + a.d_nope + 8 * m.c) * 2, y);
+      if (!b_on) return;  // uniform over the wave
+      const auto w = rotate<EX, 8>(z.wide(), sh.cs + tb * a.r.cols, sh.other, sh.buf, lane, m);
+      if (m.on && hb < a.H) C::store(a.dst + (at_group(a, t0 + tb, hb, a.d) + a.d_nope + 8 * m.c) * 2, w);
     });
-    if (d_kv > 0) {
-      const LaneMap m2(lane, d_kv / 8);
-      for_items(wave, n, (a.H + m2.per_wave - 1) / m2.per_wave, [&](int t, int hg) {
-        const int h = hg * m2.per_wave + m2.sub, col = 8 * m2.c;
-        if (!m2.on || h >= a.H) return;
-        const u32x4 x = ld_stream(a.src + ((t0 + t) * a.src_stride + (int64_t)h * d_kv + col) * 2);
-        if (col < a.d_nope) st_stream(a.dst + (at_group(a, t0 + t, h, a.d) + col) * 2, x);
-        else st_stream(a.dst2 + (at_group(a, t0 + t, h, a.d_v) + col - a.d_nope) * 2, x);
+    if (d_kv > 0)
+      move_chunks<2>(a, n, d_kv, [&](int t, int j, int k, int c, const char*& from, char*& to) {
+        from = a.src + ((t0 + t) * a.src_stride + (int64_t)(j * a.g + k) * d_kv + c) * 2;
+        const int64_t head = (j * a.T + t0 + t) * a.g + k;
+        to = c < a.d_nope ? a.dst + (head * a.d + c) * 2 : a.dst2 + (head * a.d_v + c - a.d_nope) * 2;
       });
-    }
-  }
+  });
 }
 
 // The rotation is linear and the same for all heads of a token: their gradients are summed first, then
-// rotated back once.  A wave sums a token's heads, its lanes in steps of the heads a wave holds, then over
-// those.
+// rotated back once.  One walk over dk does both: a thread keeps one chunk of a head's d columns and takes the
+// heads in steps of those that the workgroup holds at once (with few heads several tokens); it stores the chunk
+// or, of the rotated columns, adds it up.  Read in a walk of their own, those columns came at 2.8 TB/s
+// where the others came at 4.9 (16K tokens x 128 heads, fp32: 716 and 859 us).  The threads' sums are added in LDS; which
+// thread adds which heads goes by the sizes of a head and their number alone, not by the launch.
+struct SumMap {
+  int per_block, heads, tokens;  // heads that a workgroup holds at once: of one token, tokens
+  __host__ __device__ SumMap(int chunks, int H) {
+    per_block = kThreads / chunks;
+    heads = per_block < H ? per_block : H;
+    tokens = per_block / heads;
+  }
+};
 template <int EX, int IN_BYTES> __global__ __launch_bounds__(kThreads) void rope_kv_bwd_kernel(RopeArgs a) {
+  typedef Chunk<IN_BYTES> C;
+  typedef typename C::Wide Wide;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Shared sh(smem, a, wave);
-  const int d_kv = a.d_nope + a.d_v;
-  for (int64_t t0 = (int64_t)blockIdx.x * a.block_tokens; t0 < a.T; t0 += (int64_t)gridDim.x * a.block_tokens) {
-    const int n = (int)min((int64_t)a.block_tokens, a.T - t0);
-    __syncthreads();
-    fill_table(a, t0, n, sh.cs);
-    __syncthreads();
-    const LaneMap m(lane, a.r.cols / 8);
-    for (int t = wave; t < n; t += kWaves) {
-      f32x8 sum = {};
-      if (m.on)
-        for (int h = m.sub; h < a.H; h += m.per_wave) {
-          Chunk8<IN_BYTES> x;
-          x.load(a.src + (at_group(a, t0 + t, h, a.d) + a.d_nope + 8 * m.c) * IN_BYTES);
-          sum += x.wide();
+  const int d_kv = a.d_nope + a.d_v, chunks = a.d / C::N;
+  const SumMap m(chunks, a.H);
+  const int sub = threadIdx.x / chunks, c = threadIdx.x - sub * chunks, tok = sub / m.heads, first = sub - tok * m.heads;
+  const bool sums = c * C::N >= a.d_nope;
+  const int step_k = m.heads % a.g;
+  const int64_t wrap = (a.T - 1) * a.g * (int64_t)a.d * IN_BYTES;  // from one buffer's end to the next's start
+  const int64_t step = (int64_t)m.heads * a.d * IN_BYTES + (m.heads / a.g) * wrap;
+  for_blocks(a, sh, [&](int64_t t0, int n) {
+    for (int t = tok; t < n; t += m.tokens) {
+      if (tok >= m.tokens) break;
+      Wide sum = {};
+      int k = first % a.g;
+      const char* from = a.src + (at_group(a, t0 + t, first, a.d) + c * C::N) * IN_BYTES;
+      char* to = a.dst + ((t0 + t) * a.dst_stride + (int64_t)first * d_kv + c * C::N) * 2;
+      for (int h = first; h < a.H;) {
+        constexpr int U = 2;
+        C x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (h + u * m.heads < a.H) x[u].load(from);
+          from += step;
+          k += step_k;
+          if (k >= a.g) k -= a.g, from += wrap;
         }
-      wave_lds_order();
+        if (sums) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sh.buf[8 * lane + i] = sum[i];
-      wave_lds_order();
-      if (m.on && m.sub == 0)
-        for (int k = 1; k < m.per_wave; ++k)
+          for (int u = 0; u < U; ++u)
+            if (h + u * m.heads < a.H) sum += x[u].wide();
+        } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum[i] += sh.buf[8 * (lane + k * (a.r.cols / 8)) + i];
-      const f32x8 y = rotate<EX>(sum, sh.cs + t * a.r.cols, sh.other, sh.buf, lane, m);
-      if (m.on && m.sub == 0) st_stream(a.dst2 + ((t0 + t) * a.dst2_stride + 8 * m.c) * 2, narrow(y));
+          for (int u = 0; u < U; ++u)
+            if (h + u * m.heads < a.H) x[u].store(to + (int64_t)u * m.heads * d_kv * 2);
+        }
+        to += (int64_t)U * m.heads * d_kv * 2;
+        h += U * m.heads;
+      }
+      if (sums) {
+#pragma unroll
+        for (int e = 0; e < C::N; ++e) sh.part[(t * m.heads + first) * a.r.cols + c * C::N - a.d_nope + e] = sum[e];
+      }
     }
-    if (d_kv > 0) {
-      const LaneMap m2(lane, d_kv / 8);
-      for_items(wave, n, (a.H + m2.per_wave - 1) / m2.per_wave, [&](int t, int hg) {
-        const int h = hg * m2.per_wave + m2.sub, col = 8 * m2.c;
-        if (!m2.on || h >= a.H) return;
-        Chunk8<IN_BYTES> x;
-        if (col < a.d_nope) x.load(a.src + (at_group(a, t0 + t, h, a.d) + col) * IN_BYTES);
-        else x.load(a.src2 + (at_group(a, t0 + t, h, a.d_v) + col - a.d_nope) * IN_BYTES);
-        st_stream(a.dst + ((t0 + t) * a.dst_stride + (int64_t)h * d_kv + col) * 2, x.bf16());
+    if (a.d_v > 0)
+      move_chunks<IN_BYTES>(a, n, a.d_v, [&](int t, int j, int k, int col, const char*& from, char*& to) {
+        from = a.src2 + (((j * a.T + t0 + t) * a.g + k) * a.d_v + col) * IN_BYTES;
+        to = a.dst + ((t0 + t) * a.dst_stride + (int64_t)(j * a.g + k) * d_kv + a.d_nope + col) * 2;
       });
+    __syncthreads();
+    // a wave's lanes take the rotated columns of as many tokens as fit
+    const LaneMap l(lane, a.r.cols / C::N);
+    for (int i = wave * l.per_wave; i < n; i += kWaves * l.per_wave) {
+      const int t = i + l.sub;
+      const bool on = l.on && t < n;
+      Wide sum = {};
+      for (int w = 0; w < (on ? m.heads : 0); ++w)
+#pragma unroll
+        for (int e = 0; e < C::N; ++e) sum[e] += sh.part[(t * m.heads + w) * a.r.cols + C::N * l.c + e];
+      const Wide y = rotate<EX, C::N>(sum, sh.cs + min(t, n - 1) * a.r.cols, sh.other, sh.buf, lane, l);
+      if (on) C::store(a.dst2 + ((t0 + t) * a.dst2_stride + C::N * l.c) * 2, y);
     }
-  }
+  });
 }
 
 // ------------------------------------------------------------------ host side
@@ -391,23 +501,25 @@ bool any_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> i
   return false;
 }
 
-// Tokens of a workgroup: as many as give its waves a few wave-sized pieces each, and the table at most
-// 16 KB, but 2048 workgroups where there are as many tokens: what one holds in flight does not cover the
-// memory's latency.
+// Tokens of a workgroup: as few as give its waves two wave-sized pieces of rotated columns each (the fewer, the
+// more workgroups of a CU are in different phases: 16K tokens x 128 heads in one token a workgroup against
+// two: rope_kv 446 and 486 us, rope_kv_bwd 654 and 719; 32K x 16 heads in four against eight 115 and 127, 184 and
+// 187) and a thread an angle to form (64K x 2 heads in eight against four 45 and 59, 65 and 80); but 2048 workgroups
+// where there are as many tokens.
 int block_tokens(int64_t T, int H, int cols) {
   const int groups = (H + 64 / (cols / 8) - 1) / (64 / (cols / 8));
-  int n = std::max(1, std::min(32 / groups, 2048 / cols));
+  int n = std::max(1, std::min(8 / groups, 512 / cols));
   while (n > 1 && T / n < 2048) n /= 2;
   return n;
 }
 
-template <class K> int launch(K kernel, const char* name, RopeArgs& a, void* stream) {
+template <class K> int launch(K kernel, const char* name, RopeArgs& a, void* stream, int sums = 0) {
   a.block_tokens = block_tokens(a.T, a.H, a.r.cols);
   const int64_t blocks = (a.T + a.block_tokens - 1) / a.block_tokens;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int tok = prof_begin(name, s);
   hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(kThreads),
-                     shared_bytes(a.block_tokens, a.r.cols), s, a);
+                     shared_bytes(a.block_tokens, a.r.cols, sums), s, a);
   prof_end(tok, s);
   return hipGetLastError() == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
 }
@@ -423,9 +535,10 @@ int launch_kv(Exchange ex, RopeArgs& a, void* stream) {
                          : launch(rope_kv_kernel<kAnywhere>, "rope_kv", a, stream);
 }
 template <int IN_BYTES> int launch_kv_bwd(Exchange ex, RopeArgs& a, void* stream) {
-  return ex == kInChunk ? launch(rope_kv_bwd_kernel<kInChunk, IN_BYTES>, "rope_kv_bwd", a, stream)
-         : ex == kChunks ? launch(rope_kv_bwd_kernel<kChunks, IN_BYTES>, "rope_kv_bwd", a, stream)
-                         : launch(rope_kv_bwd_kernel<kAnywhere, IN_BYTES>, "rope_kv_bwd", a, stream);
+  const int sums = SumMap(a.d / Chunk<IN_BYTES>::N, a.H).heads;
+  return ex == kInChunk ? launch(rope_kv_bwd_kernel<kInChunk, IN_BYTES>, "rope_kv_bwd", a, stream, sums)
+         : ex == kChunks ? launch(rope_kv_bwd_kernel<kChunks, IN_BYTES>, "rope_kv_bwd", a, stream, sums)
+                         : launch(rope_kv_bwd_kernel<kAnywhere, IN_BYTES>, "rope_kv_bwd", a, stream, sums);
 }
 
 }  // namespace
