@@ -38,7 +38,8 @@ extern "C" {
 /* How the scores are modified.  All fields 0 or NULL, or a NULL hydra_scores_t*: not at all, and
  * the calls below are those of hydra_attn.h, on plans of either. */
 typedef struct {
-  float softcap;              /* c: 0 for none, else from 2^-10 to 2^14 and at least softmax_scale / 2^10 */
+  float softcap;              /* c: 0 for none, else from 2^-10 to 2^10, with a softmax_scale of at least 2^-8
+                                 and from 2^-14 to 2^10 times c                                */
   const float* slopes;        /* NULL for none, or DEVICE float[n_heads], finite, 4-byte aligned; read when
                                  the kernels run                                               */
   const int32_t* prefix_len;  /* NULL for none, or HOST int32[n_docs], 0 .. the document's

@@ -157,8 +157,10 @@ int check_problem(const hydra_problem_t* p, Problem* out) {
 int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out) {
   const int rc = check_problem(p, out);
   if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len)) return rc;
-  // the constants of a capped kernel hold powers of softmax_scale / cap up to the ninth
-  if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p14f && out->scale <= 0x1p10f * sc->softcap))
+  // the constants of a capped kernel are softmax_scale times powers of softmax_scale / cap up to the eighth: within
+  // these all are normal numbers
+  if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p10f && out->scale >= 0x1p-8f &&
+                              out->scale <= 0x1p10f * sc->softcap && out->scale >= 0x1p-14f * sc->softcap))
     return HYDRA_ERR_INVALID;
   if (reinterpret_cast<uintptr_t>(sc->slopes) % sizeof(float) != 0) return HYDRA_ERR_ALIGN;
   const size_t n = out->cu.size() - 1;

@@ -432,6 +432,20 @@ uint64_t turns64(double f) {
   return uint64_t((t - std::floor(t)) * 0x1p64) + uint64_t(int64_t(e * 0x1p64));
 }
 
+// Token rows (bytes): two views of one buffer, of the same stride, overlap only where their columns do.
+struct Rows {
+  const void* p;
+  uint64_t rows, stride, width;
+  Span span() const { return {p, rows > 0 && width > 0 ? (rows - 1) * stride + width : 0}; }
+};
+bool overlap(const Rows& a, const Rows& b) {
+  if (!overlap(a.span(), b.span())) return false;
+  if (a.stride != b.stride) return true;
+  const uint64_t ab = reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p);
+  const uint64_t d = ab >> 63 ? (a.stride - (0 - ab) % a.stride) % a.stride : ab % a.stride;  // b's column in a's rows
+  return !(a.width <= d && d + b.width <= a.stride);
+}
+
 // Checks and fills the table; *ex: how its pairs are exchanged.
 int make_table(const hydra_rope_t* r, RopeTable* t, Exchange* ex) {
   if (!r || r->n_axes < 1 || r->n_axes > HYDRA_ROPE_MAX_AXES) return HYDRA_ERR_INVALID;
@@ -483,9 +497,11 @@ int check_sizes(int64_t T, int H, int cp_u) {
   return HYDRA_OK;
 }
 
-int check_ptrs(std::initializer_list<const void*> ps) {
+int check_ptrs(const int32_t* positions, std::initializer_list<const void*> ps) {
+  if (!positions) return HYDRA_ERR_INVALID;
   for (const void* p : ps)
     if (!p) return HYDRA_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(positions) % sizeof(int32_t) != 0) return HYDRA_ERR_ALIGN;
   for (const void* p : ps)
     if (!aligned16(p)) return HYDRA_ERR_ALIGN;
   return HYDRA_OK;
@@ -558,7 +574,7 @@ int hydra_rope_q(const hydra_rope_t* r, int64_t n_tokens, int32_t n_heads, int32
   const int64_t width = int64_t(n_heads) * d_head;
   if (!row_stride(src_tok_stride, width, &a.src_stride)) return HYDRA_ERR_INVALID;
   if (n_tokens == 0) return HYDRA_OK;
-  if (int rc = check_ptrs({src, positions, dst}); rc != HYDRA_OK) return rc;
+  if (int rc = check_ptrs(positions, {src, dst}); rc != HYDRA_OK) return rc;
   const bool in_place = src == dst;
   if (in_place && cp_u != 1) return HYDRA_ERR_INVALID;
   const Span s = {src, rows_bytes(n_tokens, a.src_stride, width)};
@@ -589,7 +605,7 @@ int hydra_rope_q_bwd(const hydra_rope_t* r, int64_t n_tokens, int32_t n_heads, i
   const int64_t width = int64_t(n_heads) * d_head;
   if (!row_stride(src_tok_stride, width, &a.dst_stride)) return HYDRA_ERR_INVALID;
   if (n_tokens == 0) return HYDRA_OK;
-  if (int rc = check_ptrs({dq, positions, d_src}); rc != HYDRA_OK) return rc;
+  if (int rc = check_ptrs(positions, {dq, d_src}); rc != HYDRA_OK) return rc;
   if (any_overlap({{d_src, rows_bytes(n_tokens, a.dst_stride, width)}},
                   {{dq, uint64_t(n_tokens) * uint64_t(width) * uint64_t(grad_bytes)},
                    {positions, uint64_t(n_tokens) * uint64_t(r->n_axes) * 4}}))
@@ -620,8 +636,8 @@ int hydra_rope_kv(const hydra_rope_t* r, int64_t n_tokens, int32_t n_heads, int3
   if (!row_stride(kv_tok_stride, width, &a.src_stride) || !row_stride(pe_tok_stride, a.r.cols, &a.src2_stride))
     return HYDRA_ERR_INVALID;
   if (n_tokens == 0) return HYDRA_OK;
-  const void* some = positions;
-  if (int rc = check_ptrs({width > 0 ? kv : some, k_pe, positions, k, d_v > 0 ? v : some}); rc != HYDRA_OK) return rc;
+  // what is empty needs no address
+  if (int rc = check_ptrs(positions, {width > 0 ? kv : k_pe, k_pe, k, d_v > 0 ? v : k_pe}); rc != HYDRA_OK) return rc;
   const uint64_t n = uint64_t(n_tokens) * uint64_t(n_heads) * 2;
   if (any_overlap({{k, n * uint64_t(d_nope + a.r.cols)}, {d_v > 0 ? v : nullptr, n * uint64_t(d_v)}},
                   {{kv, width > 0 ? rows_bytes(n_tokens, a.src_stride, width) : 0},
@@ -658,12 +674,13 @@ int hydra_rope_kv_bwd(const hydra_rope_t* r, int64_t n_tokens, int32_t n_heads, 
   if (!row_stride(kv_tok_stride, width, &a.dst_stride) || !row_stride(pe_tok_stride, a.r.cols, &a.dst2_stride))
     return HYDRA_ERR_INVALID;
   if (n_tokens == 0) return HYDRA_OK;
-  const void* some = positions;
-  if (int rc = check_ptrs({dk, d_v > 0 ? dv : some, positions, width > 0 ? d_kv : some, d_k_pe}); rc != HYDRA_OK)
-    return rc;
+  if (int rc = check_ptrs(positions, {dk, d_v > 0 ? dv : dk, width > 0 ? d_kv : dk, d_k_pe}); rc != HYDRA_OK) return rc;
   const uint64_t n = uint64_t(n_tokens) * uint64_t(n_heads) * uint64_t(grad_bytes);
-  if (any_overlap({{d_kv, width > 0 ? rows_bytes(n_tokens, a.dst_stride, width) : 0},
-                   {d_k_pe, rows_bytes(n_tokens, a.dst2_stride, a.r.cols)}},
+  const Rows kv_rows = {d_kv, uint64_t(n_tokens), uint64_t(a.dst_stride) * 2, uint64_t(width) * 2};
+  const Rows pe_rows = {d_k_pe, uint64_t(n_tokens), uint64_t(a.dst2_stride) * 2, uint64_t(a.r.cols) * 2};
+  if (overlap(kv_rows, pe_rows)) return HYDRA_ERR_INVALID;
+  for (const Span& out : {kv_rows.span(), pe_rows.span()})
+    if (any_overlap({out},
                   {{dk, n * uint64_t(d_nope + a.r.cols)},
                    {d_v > 0 ? dv : nullptr, n * uint64_t(d_v)},
                    {positions, uint64_t(n_tokens) * uint64_t(r->n_axes) * 4}}))

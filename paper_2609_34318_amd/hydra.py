@@ -599,9 +599,11 @@ def _tok_rows(t, what: str, width: int) -> Tuple[int, int]:
     s0, *strides = t.stride()
     if math.prod(inner) != width:
         raise ValueError(f"{what}: rows of {math.prod(inner)} elements, expected {width}")
+    if not rows or not width:
+        return t.data_ptr(), 0
     step = 1
     for n, s in zip(reversed(inner), reversed(strides)):
-        if rows and n > 1 and s != step:
+        if n > 1 and s != step:
             raise ValueError(f"{what}: heads and channels must be contiguous within a token row")
         step *= n
     if rows > 1 and s0 < width:

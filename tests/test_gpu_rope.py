@@ -1,0 +1,337 @@
+"""GPU parity of the rotary calls against the fp64 oracle.
+
+A rotated value is rounded once to bf16 (at most 2^-8 of it); before that, two products and a sum in 32 bits of
+factors whose angle is within 2^-24 of a turn: 2^-20 of |a| + |b|, the magnitudes of its pair.  A gradient of k_pe sums
+H heads in 32 bits first: H roundings of 2^-24 of the sum of magnitudes.  Columns that are not rotated are
+copied (bf16) or rounded once (fp32): bit for bit."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import scores as S
+from paper_2609_34318_amd import hydra, ring
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _n(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def _close(got, want, pairs, x, extra=0.0, what=""):
+    """got within the roundings of want, x being what was rotated."""
+    a, b = pairs[0], pairs[1]
+    size = np.empty_like(x)
+    size[..., a] = size[..., b] = np.abs(x[..., a]) + np.abs(x[..., b])
+    assert np.isfinite(got).all(), what
+    bad = np.abs(got - want) > 2.0 ** -8 * np.abs(want) + (2.0 ** -20 + extra) * size
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:3])
+
+
+def _group(x, u):
+    return torch.stack(x.chunk(u, 1)).contiguous()
+
+
+CASES = [
+    # tokens, heads, cp_u, pairs, pairing, ladder, d_nope, d_v, gradients
+    (1, 1, 1, [32], "interleaved", "whole", 128, 128, F32),
+    (3, 16, 1, [32], "halves", "whole", 128, 128, F32),
+    (37, 16, 8, [32], "interleaved", "whole", 128, 128, BF16),
+    (129, 8, 2, [8, 12, 12], "axis_halves", "axis", 128, 128, F32),
+    (64, 6, 3, [8, 8, 16], "axis_halves", "axis", 128, 128, BF16),
+    (50, 5, 1, [3, 13, 16], "halves", "whole", 128, 128, BF16),
+    (33, 4, 4, [2, 2], "halves", "axis", 8, 16, F32),          # pairs whose halves are no whole chunk
+    (70, 3, 1, [4], "interleaved", "whole", 0, 0, F32),        # nothing but the rotated columns
+    (21, 2, 1, [128], "halves", "whole", 256, 0, BF16),        # the widest rotation, no values
+    (40, 7, 7, [10, 10, 10, 10], "interleaved", "axis", 40, 472, F32),
+    (2100, 1, 1, [32], "axis_halves", "whole", 128, 128, F32),  # one head: several tokens a workgroup
+    (300, 130, 2, [16, 16], "halves", "whole", 64, 64, F32),
+    (9, 300, 4, [32], "interleaved", "whole", 128, 128, F32),
+]
+
+
+class Setup:
+    def __init__(self, case, seed=0, positions=None):
+        self.T, self.H, self.u, pairs, pairing, ladder, self.dn, self.dv, self.gt = case
+        self.r = hydra.Rope(pairs, pairing, ladder=ladder)
+        self.pairs = S.rope_pairs(pairs, pairing, ladder)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        T, H, r = self.T, self.H, self.r.cols
+        self.d = self.dn + r
+        self.q, self.kv, self.pe = rnd(T, H, self.d).to(BF16), rnd(T, H, self.dn + self.dv).to(BF16), rnd(T, r).to(BF16)
+        self.dq, self.dk, self.dvv = (rnd(T, H, n).to(self.gt) for n in (self.d, self.d, self.dv))
+        self.pos = positions if positions is not None else torch.randint(-5000, 300000, (len(pairs), T), generator=g,
+                                                                         device="cuda", dtype=torch.int32)
+
+    def new(self, *shape, fill=7.0):
+        return torch.full(shape, fill, dtype=BF16, device="cuda")
+
+    def run(self):
+        T, H, u = self.T, self.H, self.u
+        q, k = self.new(u, T, H // u, self.d), self.new(u, T, H // u, self.d)
+        v = self.new(u, T, H // u, self.dv) if self.dv else None
+        hydra.rope_q(self.r, self.q, self.pos, q, cp_u=u)
+        hydra.rope_kv(self.r, self.kv, self.pe, self.pos, k, v, cp_u=u)
+        d_q, d_kv, d_pe = self.new(*self.q.shape), self.new(*self.kv.shape), self.new(*self.pe.shape)
+        hydra.rope_q_bwd(self.r, _group(self.dq, u), self.pos, d_q, cp_u=u)
+        hydra.rope_kv_bwd(self.r, _group(self.dk, u), _group(self.dvv, u) if self.dv else None, self.pos, d_kv, d_pe, cp_u=u)
+        torch.cuda.synchronize()
+        return q, k, v, d_q, d_kv, d_pe
+
+    def check(self, out):
+        q, k, v, d_q, d_kv, d_pe = out
+        dn, pos, H = self.dn, self.pos.cpu().numpy(), self.H
+        flat = lambda t: torch.cat(list(t), 1)  # noqa: E731
+        q, k = flat(q), flat(k)
+        bits = lambda a, b: torch.equal(a.view(torch.int16), b.to(BF16).view(torch.int16))  # noqa: E731
+        assert bits(q[..., :dn], self.q[..., :dn]) and bits(k[..., :dn], self.kv[..., :dn])
+        assert v is None or bits(flat(v), self.kv[..., dn:])
+        assert bits(d_q[..., :dn], self.dq[..., :dn]) and bits(d_kv[..., :dn], self.dk[..., :dn])
+        assert v is None or bits(d_kv[..., dn:], self.dvv)
+        x = _n(self.q[..., dn:])
+        _close(_n(q[..., dn:]), S.rotate(x, pos, self.pairs), self.pairs, x, what="q")
+        x = _n(self.pe)[:, None].repeat(H, 1)
+        _close(_n(k[..., dn:]), S.rotate(x, pos, self.pairs), self.pairs, x, what="k")
+        assert all(bits(k[:, h, dn:], k[:, 0, dn:]) for h in range(H))
+        x = _n(self.dq[..., dn:])
+        _close(_n(d_q[..., dn:]), S.rotate(x, pos, self.pairs, inverse=True), self.pairs, x, what="d_q")
+        x = _n(self.dk[..., dn:])
+        want = S.rotate(x.sum(1), pos, self.pairs, inverse=True)
+        _close(_n(d_pe), want, self.pairs, np.abs(x).sum(1), extra=H * 2.0 ** -24, what="d_k_pe")
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_parity(case):
+    s = Setup(CASES[case], seed=case)
+    out = s.run()
+    s.check(out)
+    assert all(a is None or torch.equal(a, b) for a, b in zip(out, s.run()))
+
+
+def test_far_positions():
+    """Both ends of int32, where 32-bit products would have lost the angle."""
+    pos = torch.tensor([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, 10 ** 9, -7, 123456789]], dtype=torch.int32, device="cuda")
+    for pairing in ("interleaved", "halves"):
+        s = Setup((9, 4, 2, [32], pairing, "whole", 128, 128, F32), positions=pos)
+        s.check(s.run())
+
+
+def test_given_frequencies():
+    """Frequencies of the caller's: negative, zero and faster than a turn a position."""
+    freq = np.concatenate([[0.0, -0.5, 7.25, -100.0, 2.0 ** 20, 1e-9], 10.0 ** -np.arange(26)])
+    s = Setup((65, 4, 1, [32], "halves", "whole", 128, 128, F32))
+    s.r = hydra.Rope([32], "halves", inv_freq=freq)
+    s.pairs = S.rope_pairs([32], "halves", inv_freq=freq)
+    s.pos.copy_(torch.arange(-30, 35, dtype=torch.int32))
+    s.check(s.run())
+
+
+def test_frequencies_of_the_library():
+    """The ladders that the library makes itself against those that the binding makes for it: a fused multiply-add
+    of difference in an angle."""
+    for ladder in ("whole", "axis"):
+        s = Setup((40, 2, 1, [8, 24], "interleaved", ladder, 128, 128, F32))
+        a = s.run()
+        s.r.c.inv_freq = None
+        b = s.run()
+        s.check(b)
+        for x, y in zip(a, b):
+            assert float((x.float() - y.float()).abs().max()) <= 2.0 ** -7 * float(x.float().abs().max())
+
+
+def test_order_of_the_sum_is_the_launch_s_no_matter():
+    """A token's sum over heads has the same bits alone and among others."""
+    for H, dt in ((1, F32), (3, F32), (16, BF16), (64, F32), (128, F32), (130, BF16)):
+        s = Setup((2500, H, 1, [32], "interleaved", "whole", 128, 128, dt))
+        full = s.run()
+        for a, n in ((0, 1), (1700, 7), (31, 600)):
+            d_kv, d_pe = s.new(n, H, 256), s.new(n, 64)
+            hydra.rope_kv_bwd(s.r, s.dk[a:a + n].contiguous(), s.dvv[a:a + n].contiguous(), s.pos[:, a:a + n].contiguous(), d_kv,
+                              d_pe)
+            torch.cuda.synchronize()
+            assert torch.equal(d_pe, full[5][a:a + n]) and torch.equal(d_kv, full[4][a:a + n])
+
+
+@pytest.mark.parametrize("pairing", ["interleaved", "halves", "axis_halves"])
+def test_in_place_and_strided_rows(pairing):
+    """In place in a fused buffer: the columns that are not rotated, and what lies between the rows, are not
+    touched; strided inputs and gradients give the dense bits."""
+    T, H = 53, 6
+    s = Setup((T, H, 1, [12, 20], pairing, "axis", 128, 128, F32))
+    want = s.run()
+    width, at = H * (192 + 256) + 64 + 16, {"q": 0, "kv": H * 192, "pe": H * 448}
+    buf = torch.randn((T, width), device="cuda").to(BF16)
+    view = lambda b, name, n, d: b[:, at[name]:at[name] + n * d].unflatten(1, (n, d)) if n > 1 else b[:, at[name]:at[name] + d]  # noqa: E731
+    q, kv, pe = view(buf, "q", H, 192), view(buf, "kv", H, 256), view(buf, "pe", 1, 64)
+    for w, t in ((q, s.q), (kv, s.kv), (pe, s.pe)):
+        w.copy_(t)
+    dense = s.new(T, H, 192)
+    hydra.rope_q(s.r, q, s.pos, dense)
+    k, v = s.new(T, H, 192), s.new(T, H, 128)
+    hydra.rope_kv(s.r, kv, pe, s.pos, k, v)
+    before = buf.clone()
+    hydra.rope_q(s.r, q, s.pos, q)
+    torch.cuda.synchronize()
+    assert torch.equal(dense, want[0][0]) and torch.equal(k, want[1][0]) and torch.equal(v, want[2][0])
+    assert torch.equal(q, want[0][0])
+    q.copy_(s.q)
+    assert torch.equal(buf, before)
+    out = torch.full((T, width), 3.0, dtype=BF16, device="cuda")
+    hydra.rope_q_bwd(s.r, s.dq, s.pos, view(out, "q", H, 192))
+    hydra.rope_kv_bwd(s.r, s.dk, s.dvv, s.pos, view(out, "kv", H, 256), view(out, "pe", 1, 64))
+    torch.cuda.synchronize()
+    for name, n, d, x in (("q", H, 192, want[3]), ("kv", H, 256, want[4]), ("pe", 1, 64, want[5])):
+        assert torch.equal(view(out, name, n, d), x)
+    assert bool((out[:, H * 448 + 64:] == 3.0).all())
+
+
+def test_no_tokens():
+    s = Setup((4, 4, 2, [32], "interleaved", "whole", 128, 128, F32))
+    e = lambda *x, dt=BF16: torch.empty(x, dtype=dt, device="cuda")  # noqa: E731
+    pos = torch.empty((1, 0), dtype=torch.int32, device="cuda")
+    hydra.rope_q(s.r, e(0, 4, 192), pos, e(2, 0, 2, 192), cp_u=2)
+    hydra.rope_kv(s.r, e(0, 4, 256), e(0, 64), pos, e(2, 0, 2, 192), e(2, 0, 2, 128), cp_u=2)
+    hydra.rope_q_bwd(s.r, e(2, 0, 2, 192, dt=F32), pos, e(0, 4, 192), cp_u=2)
+    hydra.rope_kv_bwd(s.r, e(2, 0, 2, 192, dt=F32), e(2, 0, 2, 128, dt=F32), pos, e(0, 4, 256), e(0, 64), cp_u=2)
+    torch.cuda.synchronize()
+
+
+def test_offsets_past_32_bits():
+    """90,000 tokens of 128 heads: more than 2^31 elements in q and k; sampled rows."""
+    T, H, u = 90000, 128, 8
+    s = Setup((64, H, u, [32], "halves", "whole", 128, 128, F32))
+    at = torch.cat([torch.arange(32), torch.arange(T - 32, T)]).cuda()
+    q = torch.empty((T, H, 192), dtype=BF16, device="cuda")
+    q[at] = s.q
+    pos = torch.zeros((1, T), dtype=torch.int32, device="cuda")
+    pos[:, at] = s.pos
+    out = torch.empty((u, T, H // u, 192), dtype=BF16, device="cuda")
+    hydra.rope_q(s.r, q, pos, out, cp_u=u)
+    small = s.run()
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, at], small[0])
+    back = torch.empty_like(q)
+    out[:, at] = _group(s.dq.to(BF16), u)
+    hydra.rope_q_bwd(s.r, out, pos, back, cp_u=u)
+    want = s.new(64, H, 192)
+    hydra.rope_q_bwd(s.r, _group(s.dq.to(BF16), u), s.pos, want, cp_u=u)
+    torch.cuda.synchronize()
+    assert torch.equal(back[at], want)
+
+
+def test_recorded_calls_replay():
+    s = Setup((70, 16, 4, [8, 12, 12], "axis_halves", "axis", 128, 128, F32))
+    u = s.u
+    q, k, v = s.new(u, 70, 4, 192), s.new(u, 70, 4, 192), s.new(u, 70, 4, 128)
+    d_q, d_kv, d_pe = s.new(70, 16, 192), s.new(70, 16, 256), s.new(70, 64)
+    dq, dk, dv = (_group(x, u) for x in (s.dq, s.dk, s.dvv))
+
+    def step():
+        hydra.rope_q(s.r, s.q, s.pos, q, cp_u=u)
+        hydra.rope_kv(s.r, s.kv, s.pe, s.pos, k, v, cp_u=u)
+        hydra.rope_q_bwd(s.r, dq, s.pos, d_q, cp_u=u)
+        hydra.rope_kv_bwd(s.r, dk, dv, s.pos, d_kv, d_pe, cp_u=u)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        s.q.copy_(torch.randn(s.q.shape, generator=g, device="cuda"))
+        s.pos.copy_(torch.randint(0, 1000, s.pos.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = (q, k, v, d_q, d_kv, d_pe)
+        s.check(got)
+        assert all(torch.equal(a, b) for a, b in zip(got, s.run()))
+
+
+def test_values_that_are_not_finite_stay_in_their_pair():
+    s = Setup((5, 2, 1, [32], "halves", "whole", 128, 128, F32))
+    clean = s.run()
+    s.q[2, 1, 128 + 3] = math.inf
+    s.q[2, 1, 7] = math.nan
+    q = s.run()[0]
+    bad = ~torch.isfinite(q[0].float())
+    at = {tuple(i) for i in bad.nonzero().tolist()}
+    assert at == {(2, 1, 7), (2, 1, 131), (2, 1, 163)}
+    keep = ~bad
+    assert torch.equal(q[0][keep], clean[0][0][keep])
+
+
+def test_binding_refuses_tensors():
+    s = Setup((4, 4, 2, [32], "interleaved", "whole", 128, 128, F32))
+    q = s.new(2, 4, 2, 192)
+    for args in ((s.q.cpu(), s.pos, q), (s.q.float(), s.pos, q), (s.q, s.pos.long(), q), (s.q, s.pos[:, :3], q),
+                 (s.q, s.pos, q[:, :3]), (s.q[:, :1].expand(4, 4, 192), s.pos, q),
+                 (s.q.transpose(0, 1), s.pos, q), (s.q, s.pos, q.float())):
+        with pytest.raises(ValueError):
+            hydra.rope_q(s.r, *args, cp_u=2)
+    with pytest.raises(hydra.HydraError):
+        hydra.rope_q(s.r, s.q, s.pos, s.q, cp_u=2)         # in place with several buffers
+    with pytest.raises(hydra.HydraError):
+        hydra.rope_q(s.r, s.q, s.pos, q, cp_u=3)
+    k, v = s.new(2, 4, 2, 192), s.new(2, 4, 2, 128)
+    for args in ((s.kv, s.pe[:3], s.pos, k, v), (s.kv, s.pe[:, :32], s.pos, k, v), (s.kv, s.pe, s.pos, k[..., :64], v),
+                 (s.kv, s.pe, s.pos, k, v[:, :3])):
+        with pytest.raises(ValueError):
+            hydra.rope_kv(s.r, *args, cp_u=2)
+    dk, dv = _group(s.dk, 2), _group(s.dvv, 2)
+    for args in ((dk, dv.to(BF16), s.pos, s.kv, s.pe), (dk.double(), dv, s.pos, s.kv, s.pe), (dk, dv, s.pos, s.kv, s.pe[:3]),
+                 (dk, dv, s.pos, s.kv.float(), s.pe)):
+        with pytest.raises(ValueError):
+            hydra.rope_kv_bwd(s.r, *args, cp_u=2)
+
+
+# ------------------------------------------------------------------ the layer
+
+@pytest.mark.parametrize("cap,bias,prefix,pairing", [(20.0, False, None, "interleaved"), (0.0, True, None, "halves"),
+                                                     (10.0, True, [20, 90, 0], "axis_halves"), (0.0, False, None, "halves")])
+def test_layer_between_its_projections(cap, bias, prefix, pairing):
+    """Rotation, ring share of two steps with modified scores (and with none), its backward, and the rotation's, as a
+    step runs them, against the formulas in 64 bits.  Between the parts tensors are bf16: relative L2 of the
+    gradients 3 * 2^-8 (the operands' roundings on top of the attention's)."""
+    docs, H = [50, 130, 76], 4
+    T, cu = sum(docs), [0] + list(np.cumsum(docs))
+    s = Setup((T, H, 1, [12, 20], pairing, "axis", 128, 128, F32), seed=11)
+    s.pos.copy_(torch.cat([torch.arange(n) for n in docs]).repeat(2, 1))
+    slopes = torch.tensor([0.5, 0.1, 0.02, 0.004], device="cuda") if bias else None
+    scores = hydra.Scores(cap, slopes, prefix) if cap or bias or prefix else None
+    steps = [[(0, 140)], [(140, T - 140)]]
+    sh = ring.make_share(cu, H, [(0, T)], steps, scores=scores)
+    q, k, v = s.new(T, H, 192), s.new(T, H, 192), s.new(T, H, 128)
+    hydra.rope_q(s.r, s.q, s.pos, q)
+    hydra.rope_kv(s.r, s.kv, s.pe, s.pos, k, v)
+    kv = [(k[a:a + n], v[a:a + n]) for ((a, n),) in steps]
+    ring.forward(sh, q, kv)
+    do = s.dvv.to(BF16)
+    dq = torch.zeros((T, H, 192), device="cuda")
+    dk, dv = torch.zeros((T, H, 192), device="cuda"), torch.zeros((T, H, 128), device="cuda")
+    ring.backward(sh, q, kv, do, dq, [(dk[a:a + n], dv[a:a + n]) for ((a, n),) in steps])
+    d_q, d_kv, d_pe = s.new(T, H, 192), s.new(T, H, 256), s.new(T, 64)
+    hydra.rope_q_bwd(s.r, dq, s.pos, d_q)
+    hydra.rope_kv_bwd(s.r, dk, dv, s.pos, d_kv, d_pe)
+    torch.cuda.synchronize()
+
+    pos = s.pos.cpu().numpy()
+    turn = lambda x, inv=False: np.concatenate([x[..., :128], S.rotate(x[..., 128:], pos, s.pairs, inv)], -1)  # noqa: E731
+    rq = turn(_n(s.q))
+    pe = S.rotate(_n(s.pe), pos, s.pairs)[:, None].repeat(H, 1)
+    rk, rv = np.concatenate([_n(s.kv)[..., :128], pe], -1), _n(s.kv)[..., 128:]
+    kw = dict(softcap=cap, slopes=None if slopes is None else slopes.cpu().numpy(), prefix=prefix)
+    segs = [(0, T)]
+    O, L = S.attn_fwd(rq, rk, rv, cu, segs, segs, **kw)
+    a, b, c = S.attn_bwd(rq, rk, rv, O, L, _n(do), cu, segs, segs, **kw)
+    want = (turn(a, True), np.concatenate([b[..., :128], c], -1), S.rotate(b[..., 128:].sum(1), pos, s.pairs, inverse=True))
+    assert np.abs(_n(sh.o_acc) - O).max() <= 3 * 2.0 ** -8 * np.abs(rv).max()
+    for name, x, y in zip(("d_q", "d_kv", "d_k_pe"), (d_q, d_kv, d_pe), want):
+        assert np.linalg.norm(_n(x) - y) <= 3 * 2.0 ** -8 * np.linalg.norm(y), name
