@@ -14,9 +14,9 @@
 //
 // MOD: modified scores (hydra_scores.h, scores.h); kPlain is the attention of hydra_attn.h.  A cap multiplies
 // dS by 1 - tanh^2: the dQ workgroups multiply it into dP - D, role A of dK/dV into the P that it
-// hands to role B, which needs no other.  That P is fp16 times 2^15 (P <= 1: what exceeds 2^-29 keeps 11 bits, against
-// the 8 of bf16, so that dS is rounded once to 8 bits, not twice); dS, the stored one too, and dK's
-// accumulator then hold 2^15 times their values, which the last factor takes out.
+// hands to role B, which needs no other.  That P is fp16 (11 bits against the 8 of bf16, so that dS is rounded to
+// 8 bits once, not twice).  All P of these kernels are 2^15 times their values, from a log-sum 15 less, so that
+// those above 2^-29 are normal numbers in fp16 (P <= 1); the last factor of every gradient takes that out.
 #include "kernels.h"
 #include "prof.h"
 #include "scores.h"
@@ -24,13 +24,14 @@
 namespace hydra {
 
 // ------------------------------------------------------------------ D = rowsum(dO * O)
+// and the log2 of the row's sum, less p_log2: the kernels' P are 2^p_log2 times their values.
 // O_BYTES: of O's elements, bf16 or fp32.
 template <int O_BYTES>
 __global__ __launch_bounds__(256) void bwd_pre_kernel(const void* __restrict__ o,
                                                       const uint16_t* __restrict__ dO,
                                                       const float* __restrict__ lse,
                                                       float* __restrict__ D, float* __restrict__ lse2,
-                                                      int nq, int H) {
+                                                      int nq, int H, float p_log2) {
   const int sub = threadIdx.x & 15;
   const int64_t total = (int64_t)nq * H;
   // (row, head) pairs, 16 lanes each, strided over a capped grid; the 16 lanes of a pair
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(256) void bwd_pre_kernel(const void* __restrict__ o
       const int row = (int)(rh / H), head = (int)(rh % H);
       const int64_t li = (int64_t)head * nq + row;
       D[li] = -acc;
-      lse2[li] = lse[li] * LOG2E;
+      lse2[li] = lse[li] * LOG2E - p_log2;
     }
   }
 }
@@ -242,7 +243,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
     return;
   }
   barrier_lds();  // every wave is past its last tile
-  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, a.scale, a.dq + ((int64_t)q_row0 * a.H + head) * DQK,
+  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dq + ((int64_t)q_row0 * a.H + head) * DQK,
                      a.H * DQK, q_n);
 }
 
@@ -503,7 +504,8 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             pk[2 * sb + 1] = to_bf16x8(p + 8);
             if constexpr (MOD != kPlain) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) p[e] *= (MOD & kCap) ? f[e] * P16 : P16;
+              for (int e = 0; e < 16; ++e)
+                if constexpr (MOD & kCap) p[e] *= f[e];
               lds_st16<2048 * sb>(pbuf, poff, to_f16x8(p));
               lds_st16<2048 * sb + 1024>(pbuf, poff, to_f16x8(p + 8));
             } else {
@@ -619,9 +621,9 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     barrier_lds();  // every wave is past its last tile
     const int64_t krow = (int64_t)(k_row0 + pair * 32) * a.Hkv + kv_head;
     if constexpr (ROLE == 0)
-      rows_add<DV / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, 1.0f, a.dv + krow * DV, a.Hkv * DV, kn_w);
+      rows_add<DV / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(1.0f), a.dv + krow * DV, a.Hkv * DV, kn_w);
     else
-      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, ds_scale<MOD>(a.scale), a.dk + krow * DQK, a.Hkv * DQK, kn_w);
+      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dk + krow * DQK, a.Hkv * DQK, kn_w);
   };
   if (role == 0) run(IntC<0>{});
   else run(IntC<1>{});
@@ -853,7 +855,7 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Ar
   }
 
   barrier_lds();  // every wave is past its last tile
-  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, ds_scale<MOD>(a.scale), a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
+  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
                      a.H * DQK, wave_rows ? 32 : 0);
 }
 
@@ -863,7 +865,8 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Ar
 // otherwise two of the four pairs' dV rows and three of their dK rows of a key item.
 template <bool DQ> constexpr int merge_blocks() { return DQ ? 8 * (DQK / 64) : 4 * (DV / 64 + DQK / 64); }
 
-template <bool DQ> __device__ __forceinline__ void bwd_merge_body(const AttnArgs& a, int b, lds_char* smem) {
+// unit: the factor of dV.
+template <bool DQ> __device__ __forceinline__ void bwd_merge_body(const AttnArgs& a, float unit, int b, lds_char* smem) {
   const int heads = DQ ? a.q_heads : a.kv_heads, lane = threadIdx.x;
   const int piece = b % merge_blocks<DQ>(), rest = b / merge_blocks<DQ>();
   const int hl = rest % heads;
@@ -889,14 +892,14 @@ template <bool DQ> __device__ __forceinline__ void bwd_merge_body(const AttnArgs
   }
   f32x16 acc[2];
   parts_sum(p, part_bytes, n, g, lane, [](int) { return 1.0f; }, acc);
-  rows_add<1>(smem, lane, acc, dv ? 1.0f : a.scale, out + 64 * g, pitch, rows);
+  rows_add<1>(smem, lane, acc, dv ? unit : a.scale * unit, out + 64 * g, pitch, rows);
 }
 
 // The first q_blocks workgroups merge dQ, the others dK and dV.
-__global__ __launch_bounds__(64) void bwd_merge_kernel(AttnArgs q, AttnArgs kv, int q_blocks) {
+__global__ __launch_bounds__(64) void bwd_merge_kernel(AttnArgs q, AttnArgs kv, int q_blocks, float unit) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[ROWS_OUT_BYTES];
-  if ((int)blockIdx.x < q_blocks) bwd_merge_body<true>(q, blockIdx.x, (lds_char*)smem_raw);
-  else bwd_merge_body<false>(kv, blockIdx.x - q_blocks, (lds_char*)smem_raw);
+  if ((int)blockIdx.x < q_blocks) bwd_merge_body<true>(q, unit, blockIdx.x, (lds_char*)smem_raw);
+  else bwd_merge_body<false>(kv, unit, blockIdx.x - q_blocks, (lds_char*)smem_raw);
 }
 
 namespace {
@@ -923,13 +926,12 @@ hipError_t launch_list(K kernel, const char* name, const A& a, int heads, hipStr
 
 // The merges of n_q split query items and n_kv split key items.
 template <int MOD>
-hipError_t launch_merges(const AttnArgs& q, int n_q, const AttnArgs& kv_args, int n_kv, hipStream_t stream) {
-  AttnArgs kv = kv_args;
-  kv.scale = ds_scale<MOD>(kv.scale);
+hipError_t launch_merges(const AttnArgs& q, int n_q, const AttnArgs& kv, int n_kv, hipStream_t stream) {
   const int q_blocks = n_q * q.q_heads * merge_blocks<true>(), kv_blocks = n_kv * kv.kv_heads * merge_blocks<false>();
   if (q_blocks + kv_blocks == 0) return hipSuccess;
   const int tok = prof_begin("bwd_merge", stream);
-  hipLaunchKernelGGL(bwd_merge_kernel, dim3(q_blocks + kv_blocks), dim3(64), 0, stream, q, kv, q_blocks);
+  hipLaunchKernelGGL(bwd_merge_kernel, dim3(q_blocks + kv_blocks), dim3(64), 0, stream, q, kv, q_blocks,
+                     unscaled<MOD>(1.0f));
   prof_end(tok, stream);
   return hipGetLastError();
 }
@@ -958,7 +960,7 @@ hipError_t launch_bwd(const Args<MOD>& a, int o_bytes, const Launch& q_whole, co
   const int64_t blocks = (pairs + 15) / 16 < (1 << 20) ? (pairs + 15) / 16 : (1 << 20);
   int tok = prof_begin("bwd_pre", stream);
   hipLaunchKernelGGL(o_bytes == 4 ? bwd_pre_kernel<4> : bwd_pre_kernel<2>, dim3((unsigned)blocks), dim3(256), 0,
-                     stream, a.o, a.dO, a.lse, a.Dvec, a.lse2, a.nq, a.H);
+                     stream, a.o, a.dO, a.lse, a.Dvec, a.lse2, a.nq, a.H, plain ? 0.f : P_LOG2);
   prof_end(tok, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -720,8 +720,8 @@ struct ScoreArgs : AttnArgs {
 // The polynomial of least relative error of tanh(x) / x in x^2 for |x| <= TANH_NEAR.
 constexpr double TANH_NEAR = 0.75;
 constexpr double TANH_POLY[5] = {0.99999943, -0.333282515, 0.132589832, -0.050056303, 0.0129296325};
-// P goes from role A to role B of the backward with modified scores as fp16 times this.
-constexpr float P16 = 32768.f;
+// P of the backward with modified scores is 2^P_LOG2 times its value.
+constexpr float P_LOG2 = 15.f;
 
 // What a kernel does to its scores: nothing (the plain kernels), or kScored (the prefix mask) with any of
 // the others.

@@ -175,8 +175,11 @@ __device__ __forceinline__ void score16(f32x16& s, const Args<MOD>& a, float slo
   }
 }
 
-// The factor of sums over dS (P16).
-template <int MOD> __host__ __device__ constexpr float ds_scale(float scale) { return MOD == kPlain ? scale : scale / P16; }
+// The last factor of a gradient, whose P and dS are 2^P_LOG2 times their values (exact).
+template <int MOD> __host__ __device__ constexpr float unscaled(float scale) {
+  return MOD == kPlain ? scale : scale * 0x1p-15f;
+}
+static_assert(P_LOG2 == 15.f, "unscaled");
 
 // Eight 32-bit values -> fp16, round to nearest even, in the registers of an operand fragment.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
