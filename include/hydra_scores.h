@@ -21,6 +21,10 @@
  *
  * The slopes and the cap are constants: they get no gradient.
  *
+ * Scores are formed in 32 bits: one of magnitude 2^n is off by up to 2^(n-24), which is the relative error of
+ * its weight.  A row's largest score must stay below 2^20 in magnitude (a zigzag step may see far keys alone:
+ * 2^17 rows away under a slope of 1/2 they have scores of -2^16, and weights to 2^-8); others may be lower.
+ *
  * Every convention, status code and limit is that of hydra_attn.h.  q, k and v must be finite in every
  * row, also in rows that no query sees: a masked score's weight is 0, and 0 times a value that is not
  * finite is not 0.  hydra_lse_merge merges partials of these calls too; the no-allocation call has no
@@ -71,8 +75,8 @@ int hydra_scores_fwd(const hydra_problem_t* p, const hydra_scores_t* sc, const v
  * fp32 O itself (4): dQ and dK then do not carry its rounding, which where a few keys take a row's weight
  * is more than all others together. */
 int hydra_scores_bwd(const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k, const void* v,
-                     const void* o_final, int32_t o_bytes, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
-                     float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes,
+                     const void* o_final, int32_t o_bytes, const float* lse_final, const void* d_o, float* dq_acc,
+                     float* dk_acc, float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes,
                      void* scratch, size_t scratch_bytes, int32_t planned, void* stream);
 
 #ifdef __cplusplus

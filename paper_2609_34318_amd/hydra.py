@@ -210,9 +210,16 @@ class Scores:
 
     def __init__(self, softcap: float = 0.0, slopes=None, prefix: Optional[Sequence[int]] = None):
         self.softcap, self.slopes = float(softcap), slopes
-        self.prefix = None if prefix is None else np.ascontiguousarray(np.asarray(prefix, dtype=np.int32))
+        self.prefix = None
+        if prefix is not None:
+            given = np.asarray(prefix)
+            self.prefix = np.ascontiguousarray(given.astype(np.int32))
+            if not np.array_equal(self.prefix, given):
+                raise ValueError("prefix: lengths must be integers of 32 bits")
         self.c = ScoresC()
         self.c.softcap = self.softcap
+        if self.softcap and not self.c.softcap:  # no cap to the library
+            raise ValueError(f"softcap: {self.softcap} is 0 in 32 bits")
         if slopes is not None:
             self.c.slopes = _ptr(slopes, "slopes", _F32)
         if self.prefix is not None:
@@ -387,7 +394,7 @@ def _scratch(t) -> Tuple[Optional[int], int]:
 def _fwd(what: str, merge: bool, p: Problem, q, k, v, o, lse, workspace, o_bf16, stream, planned, scratch):
     nqh = p.nq * p.n_heads
     if p.scores is not None:
-        _here(p.scores.slopes, q, k, v, o, lse, workspace)
+        _here(p.scores.slopes, q, k, v, o, lse, o_bf16, workspace, scratch)
     qp, kp, vp = _set_rows(p, q, k, v)
     _check(lib().hydra_scores_fwd(p.ref, p.scores_ref, qp, kp, vp, _ptr(o, "o", _F32, nqh * 128),
                                   _ptr(lse, "lse", _F32, nqh), _ptr(o_bf16, "o_bf16", _BF16, nqh * 128),
@@ -416,11 +423,12 @@ def _bwd(what: str, p: Problem, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc
          stream, planned, scratch):
     nqh, nkh = p.nq * p.n_heads, p.nk * p.n_kv_heads
     if p.scores is not None:
-        _here(p.scores.slopes, q, k, v, d_o, dq_acc, dk_acc, dv_acc, workspace)
+        _here(p.scores.slopes, q, k, v, o_final, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, workspace, scratch)
     qp, kp, vp = _set_rows(p, q, k, v)
     _check(lib().hydra_scores_bwd(p.ref, p.scores_ref, qp, kp, vp,
                                   _ptr(o_final, "o_final", _BF16 + _F32 if p.scores else _BF16, nqh * 128),
-                                  o_final.element_size(), _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
+                                  2 if o_final is None else o_final.element_size(),
+                                  _ptr(lse_final, "lse_final", _F32, nqh), _ptr(d_o, "d_o", _BF16, nqh * 128),
                                   _ptr(dq_acc, "dq_acc", _F32, nqh * 192), _ptr(dk_acc, "dk_acc", _F32, nkh * 192),
                                   _ptr(dv_acc, "dv_acc", _F32, nkh * 128), _ptr(ds_buf, "ds_buf"),
                                   0 if ds_buf is None else ds_buf.numel() * ds_buf.element_size(),
@@ -612,6 +620,8 @@ def _tok_rows(t, what: str, width: int) -> Tuple[int, int]:
 
 
 def _positions(r: Rope, positions, n_tokens: int) -> int:
+    if positions.shape != (r.n_axes, n_tokens) and (r.n_axes > 1 or positions.shape != (n_tokens,)):
+        raise ValueError(f"positions: shape {tuple(positions.shape)}, expected {(r.n_axes, n_tokens)}")
     return _ptr(positions, "positions", ("int32",), r.n_axes * n_tokens)
 
 
@@ -623,7 +633,7 @@ def _grad(t, what: str, n: int) -> Tuple[int, int]:
 
 def rope_q(r: Rope, src, positions, dst, cp_u: int = 1, stream=None):
     """src [T, H, d] bf16 -> dst [cp_u, T, H/cp_u, d] (cp_u = 1: also [T, H, d]) with the last r.cols columns
-    of every head rotated by positions [n_axes, T] int32.  dst may be src (cp_u = 1): in place."""
+    of every head rotated by positions [n_axes, T] (one axis: also [T]) int32.  dst may be src (cp_u = 1): in place."""
     _here(src, positions, dst)
     T, H, d = src.shape
     sp, stride = _tok_rows(src, "src", H * d)

@@ -276,6 +276,11 @@ def test_binding_refuses_tensors():
                  (s.q.transpose(0, 1), s.pos, q), (s.q, s.pos, q.float())):
         with pytest.raises(ValueError):
             hydra.rope_q(s.r, *args, cp_u=2)
+    hydra.rope_q(s.r, s.q, s.pos[0], q, cp_u=2)
+    two = hydra.Rope([16, 16])
+    for pos in (s.pos.repeat(2, 1).t().contiguous(), s.pos.repeat(1, 2), s.pos):  # of other axes first
+        with pytest.raises(ValueError, match="positions"):
+            hydra.rope_q(two, s.q, pos, q, cp_u=2)
     with pytest.raises(hydra.HydraError):
         hydra.rope_q(s.r, s.q, s.pos, s.q, cp_u=2)         # in place with several buffers
     with pytest.raises(hydra.HydraError):

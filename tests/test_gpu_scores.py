@@ -262,6 +262,18 @@ def test_plans_of_other_scores_are_refused():
     torch.cuda.synchronize()
 
 
+def test_no_rows_need_no_tensors():
+    for scores in (None, hydra.Scores(30.0)):
+        p = hydra.Problem([0, 8], 2, [], [(0, 8)], scores=scores)
+        ws = torch.empty(max(1, hydra.workspace_size(p)), dtype=torch.uint8, device="cuda")
+        k = torch.zeros((8, 2, 192), dtype=BF16, device="cuda")
+        dk = torch.ones((8, 2, 192), device="cuda")
+        dv = torch.ones((8, 2, 128), device="cuda")
+        hydra.attn_bwd(p, None, k, k[..., :128].contiguous(), None, None, None, None, dk, dv, ws)
+        torch.cuda.synchronize()
+        assert float(dk.min()) == 1 and float(dv.max()) == 1
+
+
 def test_tensors_elsewhere_are_refused():
     p = hydra.Problem([0, 8], 2, [(0, 8)], [(0, 8)], scores=hydra.Scores(30.0))
     ws = torch.empty(hydra.workspace_size(p), dtype=torch.uint8, device="cuda")

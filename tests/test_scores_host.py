@@ -242,6 +242,12 @@ def test_binding_refuses_scores():
         hydra.Scores(slopes=torch.zeros(2))
     with pytest.raises(ValueError, match="prefix"):
         hydra.Problem([0, 5, 9], 1, [(0, 9)], [(0, 9)], scores=hydra.Scores(prefix=[1]))
+    for prefix in ([1.5], [2 ** 32 + 5], np.array([2 ** 32 + 5]), [float("nan")]):
+        with pytest.raises((ValueError, OverflowError)), np.errstate(invalid="ignore"):
+            hydra.Scores(prefix=prefix)
+    for cap in (1e-46, -1e-50):  # 0 in 32 bits, which would be no cap
+        with pytest.raises(ValueError, match="softcap"):
+            hydra.Scores(softcap=cap)
     with pytest.raises(hydra.HydraError):
         ring.make_share([0, 5], 1, [(0, 5)], [[(0, 5)]], device="cpu", scores=hydra.Scores(softcap=-3.0))
 
