@@ -342,10 +342,25 @@ __global__ __launch_bounds__(128) void fwd_merge_kernel(AttnArgs a, uint16_t* __
     return *reinterpret_cast<const float2*>(p + (int64_t)j * FWD_PART_BYTES + PART_WAVE_128 + lane * 8);
   };
   float m = NEG_BIG, l = 0.f;
-#pragma unroll 4
-  for (int j = 0; j < n; ++j) m = fmax2(m, ml(j).x);
-#pragma unroll 4
-  for (int j = 0; j < n; ++j) l += __builtin_amdgcn_exp2f(ml(j).x - m) * ml(j).y;  // a part that saw nothing: l = 0
+  // the first eight parts' statistics in flight at once, and kept; past the last part: that part again, not
+  // added (a part that saw nothing: l = 0)
+  constexpr int AHEAD = 8;
+  float2 x[AHEAD];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) x[u] = ml(min(j0 + u, n - 1));
+  };
+  const int last = (n - 1) / AHEAD * AHEAD;
+  for (int j0 = last; j0 >= 0; j0 -= AHEAD) {
+    load(j0);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) m = fmax2(m, x[u].x);
+  }
+  for (int j0 = 0; j0 <= last; j0 += AHEAD) {
+    if (j0 > 0) load(j0);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) l += __builtin_amdgcn_exp2f(x[u].x - m) * (j0 + u < n ? x[u].y : 0.f);
+  }
   f32x16 acc[2];
   parts_sum(p, FWD_PART_BYTES, n, g, lane, [&](int j) { return __builtin_amdgcn_exp2f(ml(j).x - m); }, acc);
   const int q_row0 = mg[0] + 32 * wave;

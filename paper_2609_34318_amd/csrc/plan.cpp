@@ -239,10 +239,10 @@ constexpr int kCus = 256;
 // forward tile takes 1.6 to 1.7 us, a dQ tile 3.0 us, a dK/dV tile 2.5 to 2.9 us; a workgroup's own
 // cost 4 to 6 us.  A merge takes longer than it is charged, by its parts (least squares over 150
 // windows and ring steps, whole and in up to 32 parts an item: forward 4.6 us and 0.047 us a part of
-// 132 KB, dK/dV 2.4 us and 0.060 us a part of 160 KB, so up to 17 and 18 us), but charged by the part
-// the choices got worse where dQ fills the chip beside dK/dV (1.5K rows of 16 heads on 2: 81 to
-// 114 us; recompute backward over the windows 3% slower, the forward and the stored-dS backward 1%
-// faster).
+// 132 KB, dK/dV 2.4 us and 0.060 us a part of 160 KB, with a merge that waited for each part; some 40%
+// less since it holds four parts' loads ahead), but charged by the part the choices got worse where dQ
+// fills the chip beside dK/dV (1.5K rows of 16 heads on 2: 81 to 114 us; recompute backward over the
+// windows 3% slower, the forward and the stored-dS backward 1% faster).
 struct SplitCost {
   double group, merge;
 };
