@@ -186,8 +186,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
     f32x16 r[2];  // with a cap: the scores by its polynomial, while s still holds the raw ones
     if constexpr (MOD & kCap) {
       // The polynomials of the first 32 keys run under the products of the others, eight instructions (32
-      // cycles) after each (16K rows x 8 heads 740 us, behind them 788); operand reads run FWD_AHEAD k-steps
-      // ahead of their products as below.
+      // cycles) after each (16K rows x 8 heads 740 us, behind them 788; 750 to 805 since the maximum has no
+      // slack); operand reads run FWD_AHEAD k-steps ahead of their products as below.
       constexpr int N = DQK / 16;
       bf16x8 kf[2 * N];
       auto read = [&](int i) { kf[i] = op_b128<FWD_BK>(Ks, o, 32 * (i / N), i % N); };
