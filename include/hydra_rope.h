@@ -22,8 +22,8 @@
  *
  * Conventions: device pointers unless marked HOST, 16-byte aligned (positions: 4); bf16 tensors as raw
  * 16-bit patterns; token rows of inputs from projections and of their gradients are tok_stride elements
- * apart (0: dense, else at least the row's width and a multiple of 8, below 2^30), every other tensor is dense.  [G] stands for
- * send buffers [cp_u][T][H/cp_u][*] (cp_u = 1: [T][H][*]).  Arguments are checked on the host before any
+ * apart (0: dense, else at least the row's width and a multiple of 8, below 2^30), every other tensor is dense.
+ * [G] stands for send buffers [cp_u][T][H/cp_u][*] (cp_u = 1: [T][H][*]).  Arguments are checked on the host before any
  * HIP call (status codes and hydra_strerror are those of hydra_attn.h); outputs must not overlap each other
  * or an input (strided rows of one stride may be columns of one buffer).  A call enqueues one kernel on
  * `stream`, allocates nothing and writes every element of its outputs; what lies between token rows of a strided

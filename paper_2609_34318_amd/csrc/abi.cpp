@@ -17,11 +17,11 @@
 
 namespace hydra {
 hipError_t launch_attn_fwd(const AttnArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
-hipError_t launch_attn_bwd(const AttnArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                           char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
+hipError_t launch_attn_bwd(const AttnArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts,
+                           const Launch& kv, char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
 hipError_t launch_scores_fwd(const ScoreArgs& a, const Launch& l, uint16_t* o_bf16, bool merge, hipStream_t stream);
-hipError_t launch_scores_bwd(const ScoreArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                             char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
+hipError_t launch_scores_bwd(const ScoreArgs& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts,
+                             const Launch& kv, char* kv_parts, int kv_heads_per_pass, hipStream_t stream);
 hipError_t launch_lse_merge(int64_t n_rows, int H, float* o_acc, float* lse_acc, const float* o_part,
                             const float* lse_part, uint16_t* o_bf16, hipStream_t stream);
 }  // namespace hydra
@@ -261,7 +261,8 @@ namespace {
 // Forward of one ring step; `upload` = false launches only (the plan is already in the
 // workspace, from hydra_attn_plan); `merge` = true merges the partial into o_part and lse_part.
 int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const hydra_scores_t* sc, const void* q,
-                  const void* k, const void* v, float* o_part, float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, Scratch scratch, void* stream) {
+                  const void* k, const void* v, float* o_part, float* lse_part, void* o_bf16, void* workspace,
+                  size_t workspace_bytes, Scratch scratch, void* stream) {
   try {
     Problem pr;
     int rc = check_problem(p, sc, &pr);
@@ -317,9 +318,9 @@ uint64_t ds_bytes_per_head(const Problem& pr) {
 }
 
 int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* sc, const void* q, const void* k,
-                  const void* v, const void* o_final, int o_bytes, const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc,
-                  float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, Scratch scratch,
-                  void* stream, bool noalloc = false) {
+                  const void* v, const void* o_final, int o_bytes, const float* lse_final, const void* d_o,
+                  float* dq_acc, float* dk_acc, float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace,
+                  size_t workspace_bytes, Scratch scratch, void* stream, bool noalloc = false) {
   try {
     Problem pr;
     int rc = check_problem(p, sc, &pr);
@@ -425,25 +426,27 @@ int hydra_scores_bwd(const hydra_problem_t* p, const hydra_scores_t* sc, const v
                      float* dk_acc, float* dv_acc, void* ds_buf, size_t ds_bytes, void* workspace,
                      size_t workspace_bytes, void* scratch, size_t scratch_bytes, int32_t planned, void* stream) {
   if ((planned && ds_buf) || (o_bytes != 2 && o_bytes != 4)) return HYDRA_ERR_INVALID;
-  return attn_bwd_impl(planned == 0, p, sc, q, k, v, o_final, o_bytes, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
-                       workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
+  return attn_bwd_impl(planned == 0, p, sc, q, k, v, o_final, o_bytes, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf,
+                       ds_bytes, workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 
 int hydra_attn_fwd(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_part,
                    float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_fwd_impl(true, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
+  return attn_fwd_impl(true, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes,
+                       Scratch{}, stream);
 }
 
 int hydra_attn_fwd_planned(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_part,
                            float* lse_part, void* o_bf16, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_fwd_impl(false, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes, Scratch{}, stream);
+  return attn_fwd_impl(false, false, p, nullptr, q, k, v, o_part, lse_part, o_bf16, workspace, workspace_bytes,
+                       Scratch{}, stream);
 }
 
 int hydra_attn_fwd_merge(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o_acc,
                          float* lse_acc, void* o_bf16, void* workspace, size_t workspace_bytes, int32_t planned,
                          void* stream) {
-  return attn_fwd_impl(planned == 0, true, p, nullptr, q, k, v, o_acc, lse_acc, o_bf16, workspace, workspace_bytes, Scratch{},
-                       stream);
+  return attn_fwd_impl(planned == 0, true, p, nullptr, q, k, v, o_acc, lse_acc, o_bf16, workspace, workspace_bytes,
+                       Scratch{}, stream);
 }
 
 int hydra_attn_fwd_split(const hydra_problem_t* p, const void* q, const void* k, const void* v, float* o, float* lse,
@@ -456,8 +459,8 @@ int hydra_attn_fwd_split(const hydra_problem_t* p, const void* q, const void* k,
 int hydra_attn_bwd(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
                    const float* lse_final, const void* d_o, float* dq_acc, float* dk_acc, float* dv_acc,
                    void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
-                       workspace_bytes, Scratch{}, stream);
+  return attn_bwd_impl(true, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0,
+                       workspace, workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_bwd_ds(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
@@ -546,8 +549,8 @@ size_t hydra_bwd_ds_bytes(const hydra_problem_t* p, int32_t kv_heads_per_pass) {
 int hydra_attn_bwd_planned(const hydra_problem_t* p, const void* q, const void* k, const void* v,
                            const void* o_final, const float* lse_final, const void* d_o, float* dq_acc,
                            float* dk_acc, float* dv_acc, void* workspace, size_t workspace_bytes, void* stream) {
-  return attn_bwd_impl(false, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0, workspace,
-                       workspace_bytes, Scratch{}, stream);
+  return attn_bwd_impl(false, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, nullptr, 0,
+                       workspace, workspace_bytes, Scratch{}, stream);
 }
 
 int hydra_attn_bwd_split(const hydra_problem_t* p, const void* q, const void* k, const void* v, const void* o_final,
@@ -555,8 +558,8 @@ int hydra_attn_bwd_split(const hydra_problem_t* p, const void* q, const void* k,
                          void* ds_buf, size_t ds_bytes, void* workspace, size_t workspace_bytes, void* scratch,
                          size_t scratch_bytes, int32_t planned, void* stream) {
   if (planned && ds_buf) return HYDRA_ERR_INVALID;
-  return attn_bwd_impl(planned == 0, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf, ds_bytes,
-                       workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
+  return attn_bwd_impl(planned == 0, p, nullptr, q, k, v, o_final, 2, lse_final, d_o, dq_acc, dk_acc, dv_acc, ds_buf,
+                       ds_bytes, workspace, workspace_bytes, Scratch{static_cast<char*>(scratch), scratch_bytes}, stream);
 }
 
 size_t hydra_scores_scratch_size(const hydra_problem_t* p, const hydra_scores_t* sc) {

@@ -243,7 +243,8 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
     return;
   }
   barrier_lds();  // every wave is past its last tile
-  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dq + ((int64_t)q_row0 * a.H + head) * DQK,
+  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale),
+                     a.dq + ((int64_t)q_row0 * a.H + head) * DQK,
                      a.H * DQK, q_n);
 }
 
@@ -621,9 +622,11 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     barrier_lds();  // every wave is past its last tile
     const int64_t krow = (int64_t)(k_row0 + pair * 32) * a.Hkv + kv_head;
     if constexpr (ROLE == 0)
-      rows_add<DV / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(1.0f), a.dv + krow * DV, a.Hkv * DV, kn_w);
+      rows_add<DV / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(1.0f), a.dv + krow * DV,
+                        a.Hkv * DV, kn_w);
     else
-      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dk + krow * DQK, a.Hkv * DQK, kn_w);
+      rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dk + krow * DQK,
+                         a.Hkv * DQK, kn_w);
   };
   if (role == 0) run(IntC<0>{});
   else run(IntC<1>{});
@@ -855,7 +858,8 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Ar
   }
 
   barrier_lds();  // every wave is past its last tile
-  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale), a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
+  rows_add<DQK / 64>(smem + wave * ROWS_OUT_BYTES, lane_now(), acc, unscaled<MOD>(a.scale),
+                     a.dq + ((int64_t)qrow0 * a.H + head) * DQK,
                      a.H * DQK, wave_rows ? 32 : 0);
 }
 
@@ -953,8 +957,8 @@ hipError_t launch_recompute(const Args<MOD>& q, int q_merges, const Args<MOD>& k
 // Otherwise the stored-dS path, in passes of that many K/V heads (the dS of one pass's query heads
 // fits a.ds): bwd_dkdv_ds stores dS, then bwd_dq_ds reads it back.
 template <int MOD>
-hipError_t launch_bwd(const Args<MOD>& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts, const Launch& kv,
-                      char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
+hipError_t launch_bwd(const Args<MOD>& a, int o_bytes, const Launch& q_whole, const Launch& dq, char* dq_parts,
+                      const Launch& kv, char* kv_parts, int kv_heads_per_pass, hipStream_t stream) {
   constexpr bool plain = MOD == kPlain;
   const int64_t pairs = (int64_t)a.nq * a.H;
   const int64_t blocks = (pairs + 15) / 16 < (1 << 20) ? (pairs + 15) / 16 : (1 << 20);

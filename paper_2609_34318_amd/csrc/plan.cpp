@@ -8,10 +8,10 @@
 // [a, doc_end(b) - 1].  Intersecting that interval with each segment of the other chunk
 // gives at most HYDRA_MAX_SEGS contiguous ranges of local rows; anything outside them is
 // masked (Sec. 2.2) and is never visited.  With prefixes a row at p of document d sees
-// [doc_start(d), max(p + 1, prefix end(d))), whose ends grow with p too: the intervals end at the last row's
-// prefix where that is later, and a key tile that starts in a prefix is seen from its document's start.  Tiles are ordered heaviest first, the
-// kernel-level counterpart of the scheduler placing the longest sequences first
-// (Sec. 5.1.1, Alg. 1, phase 2).
+// [doc_start(d), max(p + 1, prefix end(d))), whose ends grow with p too: the intervals end at the
+// last row's prefix where that is later, and a key tile that starts in a prefix is seen from its
+// document's start.  Tiles are ordered heaviest first, the kernel-level counterpart of the scheduler
+// placing the longest sequences first (Sec. 5.1.1, Alg. 1, phase 2).
 #include "plan.h"
 
 #include "tiles.h"

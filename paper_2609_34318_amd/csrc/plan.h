@@ -85,11 +85,11 @@ void launch_units(const Problem& pr, int which, const std::vector<int32_t>& item
                   const std::vector<int32_t>& kbase, std::vector<int32_t>* units);
 
 // Byte offsets of the workspace regions, in this order: what the stored-dS backward alone reads
-// (krec, qslots), the key items, what the forward reads too (cu and with modified scores the prefix ends, qitems, and at lists the forward's
-// split list), the backward's split lists, D and LSE*log2(e).  lists holds the split lists that a plan has, one after
-// another (merges, then units); it has the same size for every problem, so that no problem needs
-// more workspace than one with more rows.  For the no-allocation call, which stores no dS and splits
-// nothing, those regions are empty.
+// (krec, qslots), the key items, what the forward reads too (cu and with modified scores the prefix
+// ends, qitems, and at lists the forward's split list), the backward's split lists, D and
+// LSE*log2(e).  lists holds the split lists that a plan has, one after another (merges, then units); it
+// has the same size for every problem, so that no problem needs more workspace than one with more rows.
+// For the no-allocation call, which stores no dS and splits nothing, those regions are empty.
 struct WsLayout {
   size_t krec_off, qslots_off, kitems_off, cu_off, qitems_off, lists_off, d_off, lse2_off, total;
   int64_t n_qitems, n_kitems;

@@ -63,7 +63,9 @@ __device__ __forceinline__ u32x4 narrow(f32x8 x) { return __builtin_bit_cast(u32
 // Loads leave their lines in the caches, where the kernel before often left them (1021 tokens x 64 heads 12 to 17 us
 // a call, 15 to 21 with the non-temporal hint; the same for tensors beyond the caches).
 __device__ __forceinline__ u32x4 ld_chunk(const char* p) { return *reinterpret_cast<const u32x4*>(p); }
-__device__ __forceinline__ void st_stream(char* p, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }
+__device__ __forceinline__ void st_stream(char* p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+}
 
 // One lane's chunk: 16 bytes of input, so that a wave's loads are contiguous, 8 columns of bf16 or 4 of fp32.
 // As it is read, as 32-bit values, and as the bf16 that is stored.
@@ -86,7 +88,8 @@ template <> struct Chunk<4> {
   __device__ __forceinline__ void store(char* p) const { store(p, wide()); }
   static __device__ __forceinline__ void store(char* p, Wide x) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), reinterpret_cast<u32x2*>(p));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)),
+                                reinterpret_cast<u32x2*>(p));
   }
 };
 

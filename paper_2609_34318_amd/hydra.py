@@ -695,8 +695,8 @@ def rope_kv_bwd(r: Rope, dk, dv, positions, d_kv, d_k_pe, cp_u: int = 1, stream=
     if d_k_pe.shape[0] != T:
         raise ValueError(f"d_k_pe: {d_k_pe.shape[0]} rows, expected {T}")
     pp, pe_stride = _tok_rows(d_k_pe, "d_k_pe", r.cols)
-    _check(lib().hydra_rope_kv_bwd(r.ref, T, H, d_nope, d_v, cp_u, gb, gp, vp, _positions(r, positions, T), dp, stride, pp,
-                                   pe_stride, _stream(stream)), "hydra_rope_kv_bwd")
+    _check(lib().hydra_rope_kv_bwd(r.ref, T, H, d_nope, d_v, cp_u, gb, gp, vp, _positions(r, positions, T), dp,
+                                   stride, pp, pe_stride, _stream(stream)), "hydra_rope_kv_bwd")
 
 
 # ------------------------------------------------------------------ scheduler (host only)
