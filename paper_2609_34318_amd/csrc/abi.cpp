@@ -220,20 +220,20 @@ AttnArgs base_args(const Problem& pr, const WsLayout& w, void* ws) {
   return a;
 }
 
-ScoreArgs score_args(const Problem& pr, const AttnArgs& base) {
+ScoreArgs score_args(const Problem& pr, const AttnArgs& base, bool backward) {
   ScoreArgs a{};
   static_cast<AttnArgs&>(a) = base;
   a.pe = base.cu + pr.cu.size();
   a.slopes = pr.slopes;
   if (pr.softcap > 0.f) {
     constexpr double log2e = 1.4426950408889634074;
-    const double in = double(pr.scale) / double(pr.softcap), out = double(pr.softcap) * log2e;
+    const double in = double(pr.scale) / double(pr.softcap), cap = double(pr.softcap) * log2e, out = backward ? 1 : cap;
     double x = in * out;
     for (int k = 0; k < 5; ++k, x *= in * in) a.poly[k] = float(TANH_POLY[k] * x);
     a.near = float(TANH_NEAR / in);
     a.two_in = float(2 * log2e * in);
     a.out = float(out);
-    a.minus_out2 = float(-1 / (out * out));
+    a.cap_log2 = float(cap);
   }
   return a;
 }
@@ -302,7 +302,7 @@ int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const hydra
     const Launch l = list_launch(workspace, w.qitems_off, w.n_qitems, plan.fwd, a.split);
     uint16_t* b = static_cast<uint16_t*>(o_bf16);
     const hipError_t e =
-        pr.scored ? launch_scores_fwd(score_args(pr, a), l, b, merge, s) : launch_attn_fwd(a, l, b, merge, s);
+        pr.scored ? launch_scores_fwd(score_args(pr, a, false), l, b, merge, s) : launch_attn_fwd(a, l, b, merge, s);
     return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
   } catch (...) {
     return HYDRA_ERR_INVALID;
@@ -380,7 +380,7 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* s
     const Launch dq = list_launch(workspace, w.qitems_off, w.n_qitems, plan.dq, dq_parts);
     const Launch kv = list_launch(workspace, w.kitems_off, w.n_kitems, plan.kv, kv_parts);
     const hipError_t e =
-        pr.scored ? launch_scores_bwd(score_args(pr, a), o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s)
+        pr.scored ? launch_scores_bwd(score_args(pr, a, true), o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s)
                   : launch_attn_bwd(a, o_bytes, q_whole, dq, dq_parts, kv, kv_parts, kv_per_pass, s);
     return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
   } catch (...) {

@@ -103,7 +103,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   const int t0 = it.t0, n_tiles = (it.t1 < 0 ? kr.nt : it.t1) - t0;  // this unit's tiles
   if (n_tiles == 0) return;  // uniform over the workgroup
   const int kv_head = head / a.grp;  // grouped K/V heads: contiguous groups of query heads
-  const float sl2 = a.scale * LOG2E;
+  const float sl2 = log2_unit<MOD>(a);
 
   // this wave's rows: [q_row0, q_row0 + q_n) at positions from q_pos0 on (q_n = 0: none)
   const int q_n = min(32, max(it.n - 32 * wave, 0));
@@ -132,7 +132,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
-  const float slope2 = slope_log2<MOD>(a, head);
+  const float slope = slope_log2<MOD>(a, head);
   settle(lse2);
   settle(neg_D);
   // With a cap the kernel needs some 14 registers more than it has: four of Q's fragments then stay in
@@ -195,13 +195,30 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
       for (int t2 = 0; t2 < DV / 16; ++t2) dp = mfma(op_b128<DQ_BK>(Vs, o, 32 * kb, t2), df[t2], dp);
 
       float ds[16];
-      if constexpr (in_log2<MOD>()) {
+      // exponent of P, and (dP - D) with the cap's factor; what slopes and a cap need is made in groups one after
+      // another, for want of registers (slopes alone: in log2 units before the log-sum, an instruction more than
+      // after it, which spills)
+      auto exponent = [&](int e) { return __builtin_fmaf(s[e], sl2, -lse2); };
+      if constexpr (MOD & kCap) {
+        float d0 = 0.f;
+        if constexpr (MOD & kBias) {
+          const int ml = lane_now();
+          d0 = float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5));
+        }
+        cap16(s, a, cap_is_far(cap_top(s), a), [&](int e0) {
+#pragma unroll
+          for (int e = e0; e < e0 + 4; ++e) {
+            dp[e] = (dp[e] + neg_D) * __builtin_fmaf(-s[e], s[e], 1.f);
+            s[e] = exponent(e);
+            if constexpr (MOD & kBias) s[e] = biased<-1>(s[e], slope, d0, e);
+          }
+          sched_fence();
+        });
+      } else if constexpr (MOD & kBias) {
         const int ml = lane_now();
-        score16<MOD, -1, true>(s, a, slope2, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)),
-                         [&](int e, float f) { dp[e] = (dp[e] + neg_D) * f; });
+        biased16<-1>(s, a.scale * LOG2E, slope, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)));
       }
-      // exponent of P, and (dP - D) with the cap's factor
-      auto arg = [&](int e) { return in_log2<MOD>() ? s[e] - lse2 : __builtin_fmaf(s[e], sl2, -lse2); };
+      auto arg = [&](int e) { return (MOD & kCap) ? s[e] : (MOD & kBias) ? s[e] - lse2 : exponent(e); };
       auto dpd = [&](int e) { return (MOD & kCap) ? dp[e] : dp[e] + neg_D; };
       if (full) {
 #pragma unroll
@@ -354,7 +371,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
   // document ends of the pair's first and last key (lanes past the end repeat the last one)
   const int hi_first = __builtin_amdgcn_readfirstlane(hi_k);
   const int hi_last = __builtin_amdgcn_readlane(hi_k, 31);
-  const float sl2 = a.scale * LOG2E;
+  const float sl2 = log2_unit<MOD>(a);
   const int qoff = dma_lane_off<DQK>(a.q_s, head0, pair, lane);  // role B's copy lanes (wave b = pair)
   const int ooff = dma_lane_off<DV>(a.H * DV, head0, pair, lane);
   const int poff = pair * (KV_NSB * 2048) + lane * 16;  // this lane's P slot: + sb*2048 + half*1024
@@ -397,7 +414,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     for (int t = 0; t < n_tiles; ++t) {
       refresh(o);
       const int qpos = cur.q.pos0, qn = cur.q.n;
-      const float slope2 = slope_log2<MOD>(a, head0 + cur.member);  // the query head's
+      const float slope = slope_log2<MOD>(a, head0 + cur.member);  // the query head's
       const int64_t ds_off = (int64_t)(ds_head0 + cur.member) * a.ds_head_bytes +
                              (int64_t)(ds_slot0 + cur.qt) * DS_TILE_BYTES;  // this tile's dS slot
       const bool more = t + 1 < n_tiles;
@@ -464,7 +481,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
           static_for<KV_BQ / 32>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
             const int qb = qpos + 32 * sb;
-            f32x16& s = sc[sb];
+            const f32x16& s = sc[sb];
             // this lane's query rows are 32*sb + 8*hh + {0..7, 16..23}
             f32x4 l0, l1, l2, l3;
             lds_x4_f32<128 * sb, 128 * sb + 16, 128 * sb + 64, 128 * sb + 80>(vec_s, 32 * hh, l0, l1, l2, l3);
@@ -474,16 +491,16 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             float p[16], f[16];
             if constexpr (MOD & kCap) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) f[e] = __builtin_fmaf(s[e] * s[e], a.minus_out2, 1.f);  // 1 - tanh^2
+              for (int e = 0; e < 16; ++e) f[e] = __builtin_fmaf(-s[e], s[e], 1.f);  // 1 - tanh^2
             }
+            float d0 = 0.f;
             if constexpr (MOD & kBias) {
               const int ml = lane_now();
-              const float d0 = float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31)));
-#pragma unroll
-              for (int e = 0; e < 16; ++e) s[e] = biased<1>((MOD & kCap) ? s[e] : s[e] * sl2, slope2, d0, e);
+              d0 = float(qb + 8 * (ml >> 5) - (k_pos0 + pair * 32 + (ml & 31)));
             }
             auto arg = [&](int e) {
-              return in_log2<MOD>() ? s[e] - lse_r[e] : __builtin_fmaf(s[e], sl2, -lse_r[e]);
+              const float x = __builtin_fmaf(s[e], sl2, -lse_r[e]);
+              return (MOD & kBias) ? biased<1>(x, slope, d0, e) : x;
             };
             if (full) {
 #pragma unroll

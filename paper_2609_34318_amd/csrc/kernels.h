@@ -716,12 +716,11 @@ struct AttnArgs {
 struct ScoreArgs : AttnArgs {
   const int* pe;        // prefix end of each document
   const float* slopes;  // [H], or null
-  // a cap c (out = 0: none), of raw scores s: c log2(e) tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to
-  // |s| = near
+  // a cap c (out = 0: none), of raw scores s: out tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to |s| = near
   float poly[5], near;
   float two_in;         // 2 log2(e) scale / c
-  float out;            // c log2(e)
-  float minus_out2;     // -1 / out^2
+  float out;            // forward c log2(e), backward 1
+  float cap_log2;       // c log2(e)
 };
 // The polynomial of least relative error of tanh(x) / x in x^2 for |x| <= TANH_NEAR.
 constexpr double TANH_NEAR = 0.75;

@@ -157,8 +157,9 @@ int check_problem(const hydra_problem_t* p, Problem* out) {
 int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out) {
   const int rc = check_problem(p, out);
   if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len)) return rc;
-  // the constants of a capped kernel are softmax_scale times powers of softmax_scale / cap up to the eighth: within
-  // these all are normal numbers
+  // the constants of a capped kernel are softmax_scale times powers of softmax_scale / cap up to the eighth (forward),
+  // and those powers up to the ninth (backward): within these all are normal numbers but the last, which has 17
+  // bits at the least and adds no more than 2^-9 of the sum
   if (sc->softcap != 0.f && !(sc->softcap >= 0x1p-10f && sc->softcap <= 0x1p10f && out->scale >= 0x1p-8f &&
                               out->scale <= 0x1p10f * sc->softcap && out->scale >= 0x1p-14f * sc->softcap))
     return HYDRA_ERR_INVALID;

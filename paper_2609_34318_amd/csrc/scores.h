@@ -1,9 +1,9 @@
 // Device-side parts of the modified scores (hydra_scores.h): what a row sees, the cap, the bias.
 //
 // The kernels hold a 32 x 32 block of raw scores in the MFMA's result registers: element e of a lane is at
-// offset 16 (e / 8) + e % 8 from the lane's first key (forward, dQ) or first query (dK/dV).  With a cap or
-// slopes the scores are turned in place into log2 units, where the plain kernels fold the scale into the
-// exponent's multiply-add.
+// offset 16 (e / 8) + e % 8 from the lane's first key (forward, dQ) or first query (dK/dV).  What is done to
+// them is counted in instructions per score: the machine runs these kernels at its power limit (1400 W), where an
+// instruction saved is time saved whether or not it was hidden behind the matrix products.
 #pragma once
 #include "kernels.h"
 
@@ -44,17 +44,24 @@ __device__ __forceinline__ Span row_span(const int* __restrict__ cu, const int* 
   return {start, max(pos + 1, prefix)};
 }
 
-// What turns raw scores into log2 units, the same for all rows of a head: the scale, or the cap's constants
-// (ScoreArgs), and the slope * log2(e).
+// The slope of a head in log2 units.
 template <int MOD> __device__ __forceinline__ float slope_log2(const Args<MOD>& a, int head) {
   if constexpr (MOD & kBias) return __int_as_float(((cint*)a.slopes)[head]) * LOG2E;
   return 0.f;
 }
-template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0; }
+template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0; }  // the forward's scores
 
-// cap * log2(e) * tanh(s * scale / cap) of raw scores s.  Up to |s| = near (TANH_NEAR caps) it is s times a
-// polynomial in s^2, of least relative error (7e-7): tanh(x) / x = P(x^2), with the caps and the scale in
-// its coefficients.  A cap is some ten times the scores it is for, so blocks that hold a score beyond that
+// The factor from what the backward has of a score (raw, or with a cap its tanh) to log2 units.
+template <int MOD> __device__ __forceinline__ float log2_unit(const Args<MOD>& a) {
+  if constexpr (MOD & kCap) return a.cap_log2;
+  else return a.scale * LOG2E;
+}
+
+// out * tanh(s * scale / cap) of raw scores s: out is cap * log2(e) in the forward, whose scores are then in log2
+// units, and 1 in the backward, which needs 1 - tanh^2 and has a multiply-add for the exponent (16K rows x
+// 8 heads, recompute backward: in log2 units there too 2467 us, so 2436).  Up to |s| = near (TANH_NEAR caps) it is s times a polynomial
+// in s^2, of least relative error (7e-7): tanh(x) / x = P(x^2), with the caps and the scale in its coefficients.  A
+// cap is some ten times the scores it is for, so blocks that hold a score beyond that
 // are few, and only for them the wave takes the exponential form, two quarter-rate instructions an element:
 // tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.
 // Four elements at a time, whose chains of dependent instructions fill each other's latency.
@@ -149,29 +156,18 @@ template <int N, class A, class P> __device__ __forceinline__ void cap_under(f32
   });
 }
 
-// The bias of an element: its distance is |d0 + DIR * (its offset)|.
-template <int DIR> __device__ __forceinline__ float biased(float s, float slope2, float d0, int e) {
-  return __builtin_fmaf(-slope2, __builtin_fabsf(d0 + DIR * float(16 * (e >> 3) + (e & 7))), s);
+// s with the bias of an element, whose distance is |d0 + DIR * (its offset)|.
+template <int DIR> __device__ __forceinline__ float biased(float s, float slope, float d0, int e) {
+  return __builtin_fmaf(-slope, __builtin_fabsf(d0 + DIR * float(16 * (e >> 3) + (e & 7))), s);
 }
 
-// 16 raw scores -> log2 units; g(e, 1 - tanh^2) for every element of a capped block.  TIGHT: element groups one
-// after another, for a kernel that has no registers for more.
-template <int MOD, int DIR, bool TIGHT, class G>
-__device__ __forceinline__ void score16(f32x16& s, const Args<MOD>& a, float slope2, float d0, G&& g) {
-  auto rest = [&](int e0) {
+// 16 raw scores -> log2 units with the bias, in groups one after another.
+template <int DIR> __device__ __forceinline__ void biased16(f32x16& s, float unit, float slope, float d0) {
 #pragma unroll
-    for (int e = e0; e < e0 + 4; ++e) {
-      if constexpr (MOD & kCap) g(e, __builtin_fmaf(s[e] * s[e], a.minus_out2, 1.f));
-      else s[e] *= a.scale * LOG2E;
-      if constexpr (MOD & kBias) s[e] = biased<DIR>(s[e], slope2, d0, e);
-    }
-    if constexpr (TIGHT) sched_fence();
-  };
-  if constexpr (MOD & kCap) {
-    cap16(s, a, cap_is_far(cap_top(s), a), rest);
-  } else {
+  for (int e0 = 0; e0 < 16; e0 += 4) {
 #pragma unroll
-    for (int e0 = 0; e0 < 16; e0 += 4) rest(e0);
+    for (int e = e0; e < e0 + 4; ++e) s[e] = biased<DIR>(s[e] * unit, slope, d0, e);
+    sched_fence();
   }
 }
 
