@@ -597,9 +597,10 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             float ds[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float pv = MOD != kPlain ? (float)__builtin_bit_cast(f16x8, pr[sb][e >> 3])[e & 7]
-                                             : (float)pr[sb][e >> 3][e & 7];
-              ds[e] = pv * dp[sb][e];
+              // fp16: a multiply-add takes it as it is (16K rows x 8 heads, prefixes: 1357 us, converted first; 1336)
+              if constexpr (MOD != kPlain)
+                ds[e] = __builtin_fmaf((float)__builtin_bit_cast(f16x8, pr[sb][e >> 3])[e & 7], dp[sb][e], 0.f);
+              else ds[e] = (float)pr[sb][e >> 3][e & 7] * dp[sb][e];
             }
             sf[sb][0] = to_bf16x8(ds);
             sf[sb][1] = to_bf16x8(ds + 8);
