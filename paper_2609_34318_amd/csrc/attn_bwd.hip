@@ -137,7 +137,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   settle(neg_D);
   // With a cap the kernel needs some 14 registers more than it has: four of Q's fragments then stay in
   // LDS behind the stages (spilled, their reloads also waited for the tile copies: 16K rows x 8 heads, recompute
-  // backward: 2682 us, spilled 2871; 2525 since P is scaled through the log-sum)
+  // backward: 2682 us, spilled 2871; 2517 with fewer instructions around them)
   constexpr int Q_LDS = (MOD & kCap) ? 4 : 0, Q_REG = DQK / 16 - Q_LDS;
   static_assert(DQ_NSTAGE * DQ_STAGE + DQ_WAVES * Q_LDS * 1024 <= DQ_LDS, "LDS");
   lds_char* q_lds = smem + DQ_NSTAGE * DQ_STAGE + wave * (Q_LDS * 1024);
@@ -449,7 +449,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
           // With a cap, a sub-block's polynomials run under the next one's products, eight instructions after
           // each, in place; one that holds scores beyond the polynomial's range (few do) is computed
           // again behind them (16K rows x 8 heads, with stored dS: 1696 us,
-          // all of them after the products 1728; 1610 since P is scaled through the log-sum)
+          // all of them after the products 1728; 1589 with fewer instructions around them)
           bool far[KV_NSB] = {};
           static_for<KV_NSB>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
