@@ -230,7 +230,10 @@ ScoreArgs score_args(const Problem& pr, const AttnArgs& base, bool backward) {
     const double in = double(pr.scale) / double(pr.softcap), cap = double(pr.softcap) * log2e, out = backward ? 1 : cap;
     double x = in * out;
     for (int k = 0; k < 5; ++k, x *= in * in) a.poly[k] = float(TANH_POLY[k] * x);
+    x = in * out;
+    for (int k = 0; k < 3; ++k, x *= in * in) a.low[k] = float(TANH_LOW[k] * x);
     a.near = float(TANH_NEAR / in);
+    a.small = float(TANH_SMALL / in);
     a.two_in = float(2 * log2e * in);
     a.out = float(out);
     a.cap_log2 = float(cap);

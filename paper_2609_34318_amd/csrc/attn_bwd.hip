@@ -137,7 +137,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   settle(neg_D);
   // With a cap the kernel needs some 14 registers more than it has: four of Q's fragments then stay in
   // LDS behind the stages (spilled, their reloads also waited for the tile copies: 16K rows x 8 heads, recompute
-  // backward: 2682 us, spilled 2871; 2517 with fewer instructions around them)
+  // backward: 2682 us, spilled 2871; 2400 with fewer instructions around them)
   constexpr int Q_LDS = (MOD & kCap) ? 4 : 0, Q_REG = DQK / 16 - Q_LDS;
   static_assert(DQ_NSTAGE * DQ_STAGE + DQ_WAVES * Q_LDS * 1024 <= DQ_LDS, "LDS");
   lds_char* q_lds = smem + DQ_NSTAGE * DQ_STAGE + wave * (Q_LDS * 1024);
@@ -205,7 +205,9 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
           const int ml = lane_now();
           d0 = float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5));
         }
-        cap16(s, a, cap_is_far(cap_top(s), a), [&](int e0) {
+        cap16<true>(s, a);
+#pragma unroll
+        for (int e0 = 0; e0 < 16; e0 += 4) {
 #pragma unroll
           for (int e = e0; e < e0 + 4; ++e) {
             dp[e] = (dp[e] + neg_D) * __builtin_fmaf(-s[e], s[e], 1.f);
@@ -213,7 +215,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
             if constexpr (MOD & kBias) s[e] = biased<-1>(s[e], slope, d0, e);
           }
           sched_fence();
-        });
+        }
       } else if constexpr (MOD & kBias) {
         const int ml = lane_now();
         biased16<-1>(s, a.scale * LOG2E, slope, float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5)));
@@ -446,37 +448,19 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
           for (int t2 = 0; t2 < DQK / 16; ++t2) qa[t2] = op_b128<KV_BQ>(qr_b, 0, t2);
           sched_fence();
           f32x16 sc[KV_NSB];
-          // With a cap, a sub-block's polynomials run under the next one's products, eight instructions after
-          // each, in place; one that holds scores beyond the polynomial's range (few do) is computed
-          // again behind them (16K rows x 8 heads, with stored dS: 1696 us,
-          // all of them after the products 1728; 1589 with fewer instructions around them)
-          bool far[KV_NSB] = {};
           static_for<KV_NSB>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;
             sc[sb] = f32x16{};
-            auto product = [&](int t2) {
+#pragma unroll
+            for (int t2 = 0; t2 < DQK / 16; ++t2) {
               sc[sb] = mfma(qa[t2], bf[t2], sc[sb]);
               if constexpr (sb + 1 < KV_NSB) qa[t2] = op_b128<KV_BQ>(qr_b, 32 * (sb + 1), t2);
-            };
-            if constexpr ((MOD & kCap) && sb > 0) {
-              far[sb - 1] = cap_is_far(cap_top(sc[sb - 1]), a);
-              cap_under<DQK / 16>(sc[sb - 1], a, product);
-            } else {
-#pragma unroll
-              for (int t2 = 0; t2 < DQK / 16; ++t2) product(t2);
             }
             sched_fence();
           });
           if constexpr (MOD & kCap) {
-            static_for<KV_NSB - 1>([&](auto sb_) {
-              constexpr int sb = decltype(sb_)::value;
-              if (!far[sb]) return;
-              sc[sb] = f32x16{};
 #pragma unroll
-              for (int t2 = 0; t2 < DQK / 16; ++t2) sc[sb] = mfma(op_b128<KV_BQ>(qr_b, 32 * sb, t2), bf[t2], sc[sb]);
-              cap16(sc[sb], a, true, [](int) {});
-            });
-            cap16(sc[KV_NSB - 1], a, cap_is_far(cap_top(sc[KV_NSB - 1]), a), [](int) {});
+            for (int sb = 0; sb < KV_NSB; ++sb) cap16<false>(sc[sb], a);
           }
           static_for<KV_BQ / 32>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;

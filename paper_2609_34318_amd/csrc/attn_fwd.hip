@@ -183,61 +183,27 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
     if (kpos >= hi_last || kpos + kn <= lo_first) continue;
 
     f32x16 s[2];
-    f32x16 r[2];  // with a cap: the scores by its polynomial, while s still holds the raw ones
-    if constexpr (MOD & kCap) {
-      // The polynomials of the first 32 keys run under the products of the others, eight instructions (32
-      // cycles) after each (16K rows x 8 heads 740 us, behind them 788; 750 to 805 since the maximum has no
-      // slack); operand reads run FWD_AHEAD k-steps ahead of their products as below.
-      constexpr int N = DQK / 16;
-      bf16x8 kf[2 * N];
-      auto read = [&](int i) { kf[i] = op_b128<FWD_BK>(Ks, o, 32 * (i / N), i % N); };
-      s[0] = f32x16{};
 #pragma unroll
-      for (int i = 0; i < FWD_AHEAD; ++i) read(i);
-      sched_fence();
-      static_for<N>([&](auto i_) {
-        constexpr int i = decltype(i_)::value;
-        s[0] = mfma(kf[i], qf[i], s[0]);
-        read(i + FWD_AHEAD);
-        sched_fence();
-      });
-      s[1] = f32x16{};
-      r[0] = s[0];
-      cap_under<N>(r[0], a, [&](int i) {
-        s[1] = mfma(kf[N + i], qf[i], s[1]);
-        if (i + FWD_AHEAD < N) read(N + i + FWD_AHEAD);
-      });
-    } else {
+    for (int kb = 0; kb < 2; ++kb) {
+      s[kb] = f32x16{};
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        s[kb] = f32x16{};
-#pragma unroll
-        for (int t2 = 0; t2 < DQK / 16; ++t2)
-          s[kb] = mfma(op_b128<FWD_BK>(Ks, o, 32 * kb, t2), qf[t2], s[kb]);
-      }
-      // operand reads six k-steps ahead of their products: left to itself the compiler runs one
-      // to two ahead, and how far changes with the code around it (256K ring step 14.29 against
-      // 14.51 ms, packed 32K 1.40 against 1.48 ms; eight ahead measures the same)
-      __builtin_amdgcn_sched_group_barrier(0x100, FWD_AHEAD, 0);
-#pragma unroll
-      for (int j = 0; j < 2 * (DQK / 16) - FWD_AHEAD; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, FWD_AHEAD, 0);
+      for (int t2 = 0; t2 < DQK / 16; ++t2)
+        s[kb] = mfma(op_b128<FWD_BK>(Ks, o, 32 * kb, t2), qf[t2], s[kb]);
     }
+    // operand reads six k-steps ahead of their products: left to itself the compiler runs one
+    // to two ahead, and how far changes with the code around it (256K ring step 14.29 against
+    // 14.51 ms, packed 32K 1.40 against 1.48 ms; eight ahead measures the same)
+    __builtin_amdgcn_sched_group_barrier(0x100, FWD_AHEAD, 0);
+#pragma unroll
+    for (int j = 0; j < 2 * (DQK / 16) - FWD_AHEAD; ++j) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, FWD_AHEAD, 0);
 
     if constexpr (MOD & kCap) {
-      cap_near16(s[1], a, r[1]);
-      if (cap_is_far(fmax2(cap_top(s[0]), cap_top(s[1])), a)) {
-        const CapConst c(a);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) r[kb][e] = cap_far(s[kb][e], r[kb][e], a, c);
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) s[kb] = r[kb];
+      for (int kb = 0; kb < 2; ++kb) cap16<false>(s[kb], a);
     }
     if constexpr (MOD & kBias) {
       const float d0 = float(q_pos0 + m - kpos - 8 * hh);  // distance of the lane's first key

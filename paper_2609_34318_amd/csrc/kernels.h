@@ -716,15 +716,19 @@ struct AttnArgs {
 struct ScoreArgs : AttnArgs {
   const int* pe;        // prefix end of each document
   const float* slopes;  // [H], or null
-  // a cap c (out = 0: none), of raw scores s: out tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to |s| = near
+  // a cap c (out = 0: none), of raw scores s: out tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to
+  // |s| = near, and s (low[0] + ...) up to |s| = small
   float poly[5], near;
+  float low[3], small;
   float two_in;         // 2 log2(e) scale / c
   float out;            // forward c log2(e), backward 1
   float cap_log2;       // c log2(e)
 };
-// The polynomial of least relative error of tanh(x) / x in x^2 for |x| <= TANH_NEAR.
+// The polynomials of least relative error of tanh(x) / x in x^2 for |x| <= TANH_NEAR and |x| <= TANH_SMALL.
 constexpr double TANH_NEAR = 0.75;
 constexpr double TANH_POLY[5] = {0.99999943, -0.333282515, 0.132589832, -0.050056303, 0.0129296325};
+constexpr double TANH_SMALL = 0.25;
+constexpr double TANH_LOW[3] = {0.9999996, -0.33321908, 0.12841613};
 // P of the backward with modified scores is 2^P_LOG2 times its value.
 constexpr float P_LOG2 = 15.f;
 

@@ -58,13 +58,14 @@ template <int MOD> __device__ __forceinline__ float log2_unit(const Args<MOD>& a
 }
 
 // out * tanh(s * scale / cap) of raw scores s: out is cap * log2(e) in the forward, whose scores are then in log2
-// units, and 1 in the backward, which needs 1 - tanh^2 and has a multiply-add for the exponent (16K rows x
-// 8 heads, recompute backward: in log2 units there too 2467 us, so 2436).  Up to |s| = near (TANH_NEAR caps) it is s times a polynomial
-// in s^2, of least relative error (7e-7): tanh(x) / x = P(x^2), with the caps and the scale in its coefficients.  A
-// cap is some ten times the scores it is for, so blocks that hold a score beyond that
-// are few, and only for them the wave takes the exponential form, two quarter-rate instructions an element:
-// tanh |x| = 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.
-// Four elements at a time, whose chains of dependent instructions fill each other's latency.
+// units, and 1 in the backward, which needs 1 - tanh^2 and has a multiply-add for the exponent (16K rows x 8 heads,
+// recompute backward: in log2 units there too 2467 us, so 2436).  tanh(x) / x is a polynomial in x^2 of least
+// relative error, with the caps and the scale in its coefficients: of three (4e-7) up to |s| = small (TANH_SMALL
+// caps), of five (6e-7) up to |s| = near (TANH_NEAR caps).  A cap is some ten times the scores it is for, so most
+// blocks of 32 x 32 take the first (forward 823 us with the second alone, 779 with both; dK/dV 1611 and 1551), and
+// few the exponential form beyond near, two quarter-rate instructions an element: tanh |x| =
+// 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.  Four elements at a time,
+// whose chains of dependent instructions fill each other's latency.
 // (The functions take any kernel's arguments, so that a plain kernel's discarded branches compile.)
 struct CapConst {
   float c4, c3, c2, c1, c0, out;
@@ -75,32 +76,32 @@ struct CapConst {
     asm volatile("" : "+s"(c3), "+s"(out));
   }
 };
-// Step K of 6 of the polynomial of s[e0 .. e0 + 3], four instructions; r after the last.
-template <int K>
-__device__ __forceinline__ void cap_step(const f32x16& s, int e0, const CapConst& c, float (&w)[4], float (&r)[4]) {
+// The polynomials of s[e0 .. e0 + 3].
+template <class A> __device__ __forceinline__ void cap_small4(const f32x16& s, int e0, const A& a, float (&r)[4]) {
+  float w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (K == 0) w[i] = s[e0 + i] * s[e0 + i];
-    if constexpr (K == 1) r[i] = __builtin_fmaf(c.c4, w[i], c.c3);
-    if constexpr (K == 2) r[i] = __builtin_fmaf(r[i], w[i], c.c2);
-    if constexpr (K == 3) r[i] = __builtin_fmaf(r[i], w[i], c.c1);
-    if constexpr (K == 4) r[i] = __builtin_fmaf(r[i], w[i], c.c0);
-    if constexpr (K == 5) r[i] *= s[e0 + i];
-  }
+  for (int i = 0; i < 4; ++i) w[i] = s[e0 + i] * s[e0 + i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(a.low[2], w[i], a.low[1]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], a.low[0]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] *= s[e0 + i];
 }
 __device__ __forceinline__ void cap_near4(const f32x16& s, int e0, const CapConst& c, float (&r)[4]) {
   float w[4];
-  static_for<6>([&](auto k) { cap_step<decltype(k)::value>(s, e0, c, w, r); });
-}
-template <class A> __device__ __forceinline__ void cap_near16(const f32x16& s, const A& a, f32x16& r) {
-  const CapConst c(a);
 #pragma unroll
-  for (int e0 = 0; e0 < 16; e0 += 4) {
-    float x[4];
-    cap_near4(s, e0, c, x);
+  for (int i = 0; i < 4; ++i) w[i] = s[e0 + i] * s[e0 + i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[e0 + i] = x[i];
-  }
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(c.c4, w[i], c.c3);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], c.c2);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], c.c1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_fmaf(r[i], w[i], c.c0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] *= s[e0 + i];
 }
 // The exponential form where |x| is beyond near, else r.
 template <class A> __device__ __forceinline__ float cap_far(float x, float r, const A& a, const CapConst& c) {
@@ -109,17 +110,23 @@ template <class A> __device__ __forceinline__ float cap_far(float x, float r, co
   settle(z);  // computed for every lane: a branch around it would be taken element by element
   return __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r;
 }
-__device__ __forceinline__ float cap_top(const f32x16& s) {
+// 16 scores of a wave's block, in place.  TIGHT: element groups one after another, for a kernel that has no
+// registers for more.
+template <bool TIGHT, class A> __device__ __forceinline__ void cap16(f32x16& s, const A& a) {
   float top = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; e += 2) top = fmax2(fmax2(top, __builtin_fabsf(s[e])), __builtin_fabsf(s[e + 1]));
-  return top;
-}
-template <class A> __device__ __forceinline__ bool cap_is_far(float top, const A& a) {
-  return __builtin_amdgcn_ballot_w64(top > a.near) != 0;
-}
-// 16 scores in place (far: cap_is_far of them, or true); done(e0) follows each group.
-template <class A, class D> __device__ __forceinline__ void cap16(f32x16& s, const A& a, bool far, D&& done) {
+  if (__builtin_amdgcn_ballot_w64(top > a.small) == 0) {
+#pragma unroll
+    for (int e0 = 0; e0 < 16; e0 += 4) {
+      float r[4];
+      cap_small4(s, e0, a, r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
+    }
+    return;
+  }
+  const bool far = __builtin_amdgcn_ballot_w64(top > a.near) != 0;
   const CapConst c(a);
 #pragma unroll
   for (int e0 = 0; e0 < 16; e0 += 4) {
@@ -131,29 +138,8 @@ template <class A, class D> __device__ __forceinline__ void cap16(f32x16& s, con
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
-    done(e0);
+    if constexpr (TIGHT) sched_fence();
   }
-}
-// 16 near scores in place, by the polynomial, under N = 12 products: product(i) starts the i-th, and eight
-// instructions (32 cycles) follow each.  The fences keep the compiler from moving them behind all products.
-template <int N, class A, class P> __device__ __forceinline__ void cap_under(f32x16& s, const A& a, P&& product) {
-  static_assert(N == 12, "four groups of six steps");
-  const CapConst c(a);
-  float w[4], r[4];
-  static_for<N>([&](auto i_) {
-    constexpr int i = decltype(i_)::value;
-    product(i);
-    cap_step<2 * (i % 3)>(s, 4 * (i / 3), c, w, r);
-    cap_step<2 * (i % 3) + 1>(s, 4 * (i / 3), c, w, r);
-    if constexpr (i % 3 == 2) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        settle(r[e]);  // here, not where it is first used
-        s[4 * (i / 3) + e] = r[e];
-      }
-    }
-    sched_fence();
-  });
 }
 
 // s with the bias of an element, whose distance is |d0 + DIR * (its offset)|.

@@ -323,20 +323,21 @@ def test_binding_refuses_rope_tensors():
 
 def test_polynomial_of_the_cap():
     """s (poly[0] + poly[1] s^2 + ...) in 32 bits, as the kernels evaluate it, against out tanh(s scale / c), where out
-    is c log2(e) in the forward and 1 in the backward: seven roundings of half a step each on top of the fit's 6e-7, over scores up to the polynomial's range."""
+    is c log2(e) in the forward and 1 in the backward, and the shorter one of small scores: seven roundings of half a step each on top of the fit's 6e-7, over scores up to the polynomial's range."""
     text = open(os.path.join(CSRC, "kernels.h")).read()
-    poly = [float(x) for x in re.search(r"TANH_POLY\[5\] = \{(.*?)\}", text).group(1).split(",")]
-    near = float(re.search(r"TANH_NEAR = ([0-9.]+)", text).group(1))
+    numbers = lambda name: [float(x) for x in re.search(name + r" = \{?(.*?)\}?;", text).group(1).split(",")]  # noqa: E731
     f = np.float32
     for cap, scale in ((50.0, 192 ** -0.5), (30.0, 1.0), (2.0 ** 10, 2.0 ** -4), (2.0 ** -10, 1.0), (2.0 ** 6, 2.0 ** -8),
                        (2.0 ** 10, 2.0 ** 20)):
         into = scale / cap
-        for out in (cap * math.log2(math.e), 1.0):
-            c = [f(poly[k] * into * out * into ** (2 * k)) for k in range(5)]
+        for out, name, n, end in ((cap * math.log2(math.e), "TANH_POLY", 5, "TANH_NEAR"), (1.0, "TANH_POLY", 5, "TANH_NEAR"),
+                                  (cap * math.log2(math.e), "TANH_LOW", 3, "TANH_SMALL"), (1.0, "TANH_LOW", 3, "TANH_SMALL")):
+            poly, (near,) = numbers(name + rf"\[{n}\]"), numbers(end)
+            c = [f(poly[k] * into * out * into ** (2 * k)) for k in range(n)]
             s = np.linspace(0, near / into, 20001)[1:].astype(f)
             w = s * s
-            r = f(c[4]) * w + f(c[3])
-            for k in (2, 1, 0):
+            r = f(c[n - 1]) * w + f(c[n - 2])
+            for k in reversed(range(n - 2)):
                 r = r * w + f(c[k])
             got = (r * s).astype(np.float64)
             want = out * np.tanh(s.astype(np.float64) * into)
