@@ -205,7 +205,7 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
           const int ml = lane_now();
           d0 = float(q_pos0 + (ml & 31) - kpos - 32 * kb - 8 * (ml >> 5));
         }
-        cap16<true>(s, a);
+        cap_blocks<true, 1>(&s, a);
 #pragma unroll
         for (int e0 = 0; e0 < 16; e0 += 4) {
 #pragma unroll
@@ -459,8 +459,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             sched_fence();
           });
           if constexpr (MOD & kCap) {
-#pragma unroll
-            for (int sb = 0; sb < KV_NSB; ++sb) cap16<false>(sc[sb], a);
+            cap_blocks<false, KV_NSB>(sc, a);
           }
           static_for<KV_BQ / 32>([&](auto sb_) {
             constexpr int sb = decltype(sb_)::value;

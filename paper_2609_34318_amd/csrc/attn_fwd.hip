@@ -203,7 +203,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
 
     if constexpr (MOD & kCap) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) cap16<false>(s[kb], a);
+      for (int kb = 0; kb < 2; ++kb) cap_blocks<false, 1>(s + kb, a);
     }
     if constexpr (MOD & kBias) {
       const float d0 = float(q_pos0 + m - kpos - 8 * hh);  // distance of the lane's first key

@@ -110,35 +110,48 @@ template <class A> __device__ __forceinline__ float cap_far(float x, float r, co
   settle(z);  // computed for every lane: a branch around it would be taken element by element
   return __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r;
 }
-// 16 scores of a wave's block, in place.  TIGHT: element groups one after another, for a kernel that has no
-// registers for more.
-template <bool TIGHT, class A> __device__ __forceinline__ void cap16(f32x16& s, const A& a) {
-  float top = 0.f;
+// A wave's blocks of 16 scores a lane, in place.  TIGHT: element groups one after another, for a kernel that has
+// no registers for more.
+template <bool TIGHT, int N, class A> __device__ __forceinline__ void cap_blocks(f32x16* s, const A& a) {
+  float top[N];
 #pragma unroll
-  for (int e = 0; e < 16; e += 2) top = fmax2(fmax2(top, __builtin_fabsf(s[e])), __builtin_fabsf(s[e + 1]));
-  if (__builtin_amdgcn_ballot_w64(top > a.small) == 0) {
+  for (int n = 0; n < N; ++n) {
+    top[n] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2)
+      top[n] = fmax2(fmax2(top[n], __builtin_fabsf(s[n][e])), __builtin_fabsf(s[n][e + 1]));
+  }
+  float t = top[0];
+#pragma unroll
+  for (int n = 1; n < N; ++n) t = fmax2(t, top[n]);
+  if (__builtin_amdgcn_ballot_w64(t > a.small) == 0) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e0 = 0; e0 < 16; e0 += 4) {
+        float r[4];
+        cap_small4(s[n], e0, a, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][e0 + i] = r[i];
+      }
+    return;
+  }
+  const CapConst c(a);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const bool far = __builtin_amdgcn_ballot_w64(top[n] > a.near) != 0;
 #pragma unroll
     for (int e0 = 0; e0 < 16; e0 += 4) {
       float r[4];
-      cap_small4(s, e0, a, r);
+      cap_near4(s[n], e0, c, r);
+      if (far) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
+        for (int i = 0; i < 4; ++i) r[i] = cap_far(s[n][e0 + i], r[i], a, c);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][e0 + i] = r[i];
+      if constexpr (TIGHT) sched_fence();
     }
-    return;
-  }
-  const bool far = __builtin_amdgcn_ballot_w64(top > a.near) != 0;
-  const CapConst c(a);
-#pragma unroll
-  for (int e0 = 0; e0 < 16; e0 += 4) {
-    float r[4];
-    cap_near4(s, e0, c, r);
-    if (far) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = cap_far(s[e0 + i], r[i], a, c);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[e0 + i] = r[i];
-    if constexpr (TIGHT) sched_fence();
   }
 }
 
