@@ -110,8 +110,9 @@ template <class A> __device__ __forceinline__ float cap_far(float x, float r, co
   settle(z);  // computed for every lane: a branch around it would be taken element by element
   return __builtin_fabsf(x) > a.near ? __builtin_copysignf(z, x) : r;
 }
-// A wave's blocks of 16 scores a lane, in place.  TIGHT: element groups one after another, for a kernel that has
-// no registers for more.
+// A wave's blocks of 16 scores a lane, in place, masked ones among them.  A lane that holds a NaN (a masked pair whose
+// products overflow to infinities of both signs) takes the general form, for it may hold any score besides.
+// TIGHT: element groups one after another, for a kernel that has no registers for more.
 template <bool TIGHT, int N, class A> __device__ __forceinline__ void cap_blocks(f32x16* s, const A& a) {
   float top[N];
 #pragma unroll
@@ -124,7 +125,7 @@ template <bool TIGHT, int N, class A> __device__ __forceinline__ void cap_blocks
   float t = top[0];
 #pragma unroll
   for (int n = 1; n < N; ++n) t = fmax2(t, top[n]);
-  if (__builtin_amdgcn_ballot_w64(t > a.small) == 0) {
+  if (__builtin_amdgcn_ballot_w64(!(t <= a.small)) == 0) {
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -139,7 +140,7 @@ template <bool TIGHT, int N, class A> __device__ __forceinline__ void cap_blocks
   const CapConst c(a);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const bool far = __builtin_amdgcn_ballot_w64(top[n] > a.near) != 0;
+    const bool far = __builtin_amdgcn_ballot_w64(!(top[n] <= a.near)) != 0;
 #pragma unroll
     for (int e0 = 0; e0 < 16; e0 += 4) {
       float r[4];
