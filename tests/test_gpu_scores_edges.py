@@ -45,6 +45,21 @@ def test_masked_scores_that_overflow(which, mod):
     _check_forward(s, sh, O, L, which)
 
 
+@pytest.mark.parametrize("ds", [False, True])
+@pytest.mark.parametrize("mod", MODS)
+@pytest.mark.parametrize("which", ["keys", "queries"])
+def test_gradients_beside_masked_scores_that_overflow(which, mod, ds):
+    s = _overflowing(which, mod)
+    _, _, rq, rkv = s.reference()
+    sh = s.share(ds)
+    assert (sh.ds_buf is not None) == ds
+    ring.forward(sh, s.q, s.kv)
+    dq, dkv = s.grads()
+    ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+    torch.cuda.synchronize()
+    _check_grads((dq, dkv), (rq, rkv), which)
+
+
 def _poison(value):
     """Forward and both backwards over 512 rows x 256 heads of `value`, more workgroups than CUs."""
     n, H = 512, 256
