@@ -44,9 +44,10 @@ __device__ __forceinline__ Span row_span(const int* __restrict__ cu, const int* 
   return {start, max(pos + 1, prefix)};
 }
 
-// The slope of a head in log2 units.
+// The slope of a head in log2 units, finite: an infinite one times the distance 0 of a row's own key is NaN.
 template <int MOD> __device__ __forceinline__ float slope_log2(const Args<MOD>& a, int head) {
-  if constexpr (MOD & kBias) return __int_as_float(((cint*)a.slopes)[head]) * LOG2E;
+  if constexpr (MOD & kBias)
+    return __builtin_amdgcn_fmed3f(__int_as_float(((cint*)a.slopes)[head]) * LOG2E, -0x1.fffffep127f, 0x1.fffffep127f);
   return 0.f;
 }
 template <int MOD> constexpr bool in_log2() { return (MOD & (kCap | kBias)) != 0; }  // the forward's scores

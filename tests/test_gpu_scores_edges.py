@@ -1,4 +1,5 @@
-"""What modified scores may not depend on: masked pairs whose scores overflow, and rows that a short tile leaves in LDS.
+"""Edges of the modified scores: masked pairs whose scores overflow, rows that a short tile leaves in LDS, slopes at the
+ends of their range.
 
 The cap takes a shorter polynomial where all scores of a block are small.  A masked pair's score may be NaN (finite
 values whose products overflow to both infinities) and must not hide a score of its block that is beyond the
@@ -107,3 +108,21 @@ def test_rows_left_in_lds(case, mod):
             if first is None:
                 first = out
             assert all(torch.equal(a, b) for a, b in zip(first, out)), (ds, value)
+
+
+def test_slopes_at_the_ends_of_their_range():
+    """Slopes whose multiple of log2(e) is beyond 32 bits: a row's own key, at distance 0, is all it sees, and the next
+    one where the head's slope is 0."""
+    n, most = 70, torch.finfo(torch.float32).max
+    for mod in ("bias", "all_no_prefix"):
+        s = Setup(([n], 3, 1, [(0, n)], [[(0, n)]]), mod, seed=13)
+        s.slopes.copy_(torch.tensor([most, 2.4e38, 0.0]))
+        O, L, rq, rkv = s.reference()
+        sh = s.share()
+        ring.forward(sh, s.q, s.kv)
+        _check_forward(s, sh, O, L, mod)
+        dq, dkv = s.grads()
+        ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+        torch.cuda.synchronize()
+        assert torch.equal(sh.o_acc[:, :2], s.kv[0][1].float().expand(-1, 2, -1))
+        _check_grads((dq, dkv), (rq, rkv), mod)
