@@ -21,9 +21,13 @@
  *
  * The slopes and the cap are constants: they get no gradient.
  *
- * Scores are formed in 32 bits: one of magnitude 2^n is off by up to 2^(n-24), which is the relative error of
- * its weight.  A row's largest score must stay below 2^20 in magnitude (a zigzag step may see far keys alone:
- * 2^17 rows away under a slope of 1/2 they have scores of -2^16, and weights to 2^-8); others may be lower.
+ * Scores are formed in 32 bits.  With A = softmax_scale sum_c |q_ic k_jc|, s the (capped) score before its bias and
+ * B = |slope_h (p_i - p_j)|, one is off by at most 2^-16 A + 2^-21 (|s| + B), with a cap by 2^-19 |s| besides, and its
+ * weight by that much of itself; the factor 1 - t^2 is off by up to 2^-20.  tanh is a polynomial whose length is
+ * chosen for a block of scores (32 x 32, in dK/dV 96 x 32) by its largest, masked ones included: within these bounds
+ * a capped row's results depend on the rows and keys beside it in the window, and are not the same bits in another.
+ * A row's largest score must stay below 2^20 in magnitude (a zigzag step may see far keys alone: 2^17 rows away under
+ * a slope of 1/2 they have scores of -2^16, and weights to 2^-5); others may be lower.
  *
  * Every convention, status code and limit is that of hydra_attn.h.  q, k and v must be finite in every
  * row, also in rows that no query sees: a masked score's weight is 0, and 0 times a value that is not

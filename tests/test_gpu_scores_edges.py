@@ -126,3 +126,46 @@ def test_slopes_at_the_ends_of_their_range():
         torch.cuda.synchronize()
         assert torch.equal(sh.o_acc[:, :2], s.kv[0][1].float().expand(-1, 2, -1))
         _check_grads((dq, dkv), (rq, rkv), mod)
+
+# ------------------------------------------------------------------ how far a score may be off
+
+def _key_scores(q, k, scale, cap, slopes):
+    """The score of every row against key 0 of its document, which is its LSE where it sees that key alone; and in 64 bits
+    A (the products' magnitudes summed), the capped score and the bias."""
+    n, H = q.shape[:2]
+    p = hydra.Problem([0, n], H, [(0, n)], [(0, 1)], softmax_scale=scale, n_kv_heads=1,
+                      scores=hydra.Scores(cap, slopes, None if cap or slopes is not None else [0]))
+    ws = torch.empty(hydra.workspace_size(p), dtype=torch.uint8, device="cuda")
+    o, lse = torch.empty((n, H, 128), device="cuda"), torch.empty((H, n), device="cuda")
+    hydra.attn_fwd(p, q, k, torch.zeros((1, 1, 128), dtype=BF16, device="cuda"), o, lse, ws)
+    torch.cuda.synchronize()
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    tau = float(np.float32(scale))
+    terms = f(q) * f(k)[:, 0]
+    A, s = tau * np.abs(terms).sum(-1).T, tau * terms.sum(-1).T
+    if cap:
+        s = cap * np.tanh(s / cap)
+    B = np.zeros((H, n)) if slopes is None else f(slopes)[:, None] * np.arange(n)[None]
+    return f(lse), A, s, B
+
+
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("cap,scale,size", [(0.0, 192 ** -0.5, 1.0), (0.0, 0.25, 1000.0), (50.0, 192 ** -0.5, 8.0),
+                                            (1024.0, 0.25, 60.0), (2.0 ** -10, 0.25, 0.01), (30.0, 1.0, 1.0)])
+@pytest.mark.parametrize("columns", [1, 192])
+def test_scores_are_as_near_as_stated(columns, cap, scale, size, biased):
+    """hydra_scores.h: off by at most 2^-16 A + 2^-21 (|s| + B), with a cap by 2^-19 |s| besides.  192 sums that are off
+    by half a step, 2^-24, of at most A: 192 2^-24 < 2^-16 of A; none where all columns but one are 0, whose product is
+    exact.  Behind them lie at most seven roundings of s (scale times log2 e and that constant, the product, the bias'
+    multiply-add, ln 2 and its product in the LSE, and one to spare) and as many of the bias (slope times log2 e and that
+    constant, the distance, the multiply-add, ln 2 and its product): less than 8 2^-24 of each.  tanh: the polynomial's
+    6e-7 and seven roundings of 2^-24, less than 2^-19."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    n, H = 700, 4
+    q = torch.randn((n, H, 192), generator=g, device="cuda") * size
+    k = torch.randn((1, 1, 192), generator=g, device="cuda")
+    q[..., columns:] = 0
+    slopes = torch.tensor([0.5, 0.01, 1e-4, 3.0], device="cuda") if biased else None
+    lse, A, s, B = _key_scores(q.to(BF16), k.to(BF16), scale, cap, slopes)
+    allowed = 2.0 ** -21 * (np.abs(s) + B) + (2.0 ** -19 * np.abs(s) if cap else 0) + (2.0 ** -16 * A if columns > 1 else 0)
+    assert (np.abs(lse - (s - B)) <= allowed).all()
