@@ -63,7 +63,9 @@ int64_t hydra_scores_visible_pairs(const hydra_problem_t* p, const hydra_scores_
 int64_t hydra_scores_plan_items(const hydra_problem_t* p, const hydra_scores_t* sc, int32_t which, int32_t* out,
                                 int64_t cap);
 
-/* hydra_attn_plan: the plan depends on the prefixes, not on the cap or the slopes. */
+/* hydra_attn_plan: the plan, and the workspace's size, depend on the prefixes (NULL is 0 for every document) and on
+ * whether the scores are modified at all, not on the cap or the slopes: planned calls may turn either on, off or to
+ * another value on one plan, but not the last modification off or the first one on (HYDRA_ERR_WORKSPACE). */
 int hydra_scores_plan(const hydra_problem_t* p, const hydra_scores_t* sc, void* workspace, size_t workspace_bytes,
                       void* stream);
 
