@@ -578,7 +578,7 @@ class Rope:
             inv_freq = [base ** -(j / m if ladder == "axis" else (j + j0) / n)
                         for m, j0 in zip(pairs, [sum(pairs[:a]) for a in range(len(pairs))]) for j in range(m)]
         if inv_freq is not None:
-            self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
+            self.inv_freq = np.array(inv_freq, dtype=np.float64, order="C")  # a copy: the library reads it in every call
             if self.inv_freq.shape != (sum(pairs),):
                 raise ValueError(f"inv_freq: shape {self.inv_freq.shape}, expected {(sum(pairs),)}")
             self.c.inv_freq = self.inv_freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
