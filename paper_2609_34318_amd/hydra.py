@@ -573,7 +573,7 @@ class Rope:
         self.c.pairing = self.PAIRINGS.index(pairing)
         self.c.per_axis = int(ladder == "axis")
         self.c.base = base
-        if inv_freq is None and base >= 1:  # made once here, not in every call (the library refuses other bases)
+        if inv_freq is None and 1 <= base < math.inf:  # made once here, not in every call (the library refuses other bases)
             n = sum(pairs)
             inv_freq = [base ** -(j / m if ladder == "axis" else (j + j0) / n)
                         for m, j0 in zip(pairs, [sum(pairs[:a]) for a in range(len(pairs))]) for j in range(m)]

@@ -1,4 +1,6 @@
 """hydra.Rope on the host: what it keeps of its arguments."""
+import math
+
 import numpy as np
 
 from paper_2609_34318_amd import hydra
@@ -13,3 +15,13 @@ def test_given_frequencies_are_copied():
     assert np.array_equal(r.inv_freq, want) and [r.c.inv_freq[j] for j in range(32)] == list(want)
     back = hydra.Rope(inv_freq=want[::-1])
     assert [back.c.inv_freq[j] for j in range(32)] == list(want[::-1])
+
+
+def test_bases_that_the_library_refuses():
+    """An infinite base would turn the first pair by one radian per position and no other; the library refuses it, and
+    every other base that is not at least 1."""
+    for base in (math.inf, math.nan, 0.5, 0.0, -10000.0):
+        for ladder in ("whole", "axis"):
+            r = hydra.Rope(base=base, ladder=ladder)
+            assert hydra.lib().hydra_rope_q(r.ref, 0, 8, 192, 1, None, 0, None, None, None) == -1, base
+    assert hydra.lib().hydra_rope_q(hydra.Rope(base=1).ref, 0, 8, 192, 1, None, 0, None, None, None) == 0
