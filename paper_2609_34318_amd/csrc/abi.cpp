@@ -40,23 +40,31 @@ std::vector<ProfRec> g_prof;
 }  // namespace
 
 namespace hydra {
-int prof_begin(const char* kernel, hipStream_t stream) {
-  std::lock_guard<std::mutex> lock(g_prof_mu);
-  if (!g_prof_on) return -1;
-  ProfRec r{kernel, nullptr, nullptr};
-  if (hipEventCreate(&r.start) != hipSuccess) return -1;
-  if (hipEventCreate(&r.stop) != hipSuccess) {
-    (void)hipEventDestroy(r.start);
+int prof_begin(const char* kernel, hipStream_t stream) noexcept {
+  try {
+    std::lock_guard<std::mutex> lock(g_prof_mu);
+    if (!g_prof_on) return -1;
+    g_prof.emplace_back();  // before the events, which a throw here would lose
+    ProfRec r{kernel, nullptr, nullptr};
+    if (hipEventCreate(&r.start) != hipSuccess || hipEventCreate(&r.stop) != hipSuccess) {
+      if (r.start) (void)hipEventDestroy(r.start);
+      g_prof.pop_back();
+      return -1;
+    }
+    (void)hipEventRecord(r.start, stream);
+    g_prof.back() = r;
+    return int(g_prof.size()) - 1;
+  } catch (...) {
     return -1;
   }
-  (void)hipEventRecord(r.start, stream);
-  g_prof.push_back(r);
-  return int(g_prof.size()) - 1;
 }
-void prof_end(int token, hipStream_t stream) {
+void prof_end(int token, hipStream_t stream) noexcept {
   if (token < 0) return;
-  std::lock_guard<std::mutex> lock(g_prof_mu);
-  if (token < int(g_prof.size())) (void)hipEventRecord(g_prof[token].stop, stream);
+  try {
+    std::lock_guard<std::mutex> lock(g_prof_mu);
+    if (token < int(g_prof.size())) (void)hipEventRecord(g_prof[size_t(token)].stop, stream);
+  } catch (...) {
+  }
 }
 }  // namespace hydra
 
@@ -644,44 +652,52 @@ int64_t hydra_plan_items(const hydra_problem_t* p, int32_t which, int32_t* out, 
 }
 
 int hydra_profile_start(void) {
-  std::lock_guard<std::mutex> lock(g_prof_mu);
-  prof_clear_locked();
-  g_prof_on = true;
-  return HYDRA_OK;
+  try {
+    std::lock_guard<std::mutex> lock(g_prof_mu);
+    prof_clear_locked();
+    g_prof_on = true;
+    return HYDRA_OK;
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
+  }
 }
 
 int hydra_profile_stop(hydra_kernel_stat_t* out, int32_t cap) {
-  std::lock_guard<std::mutex> lock(g_prof_mu);
-  g_prof_on = false;
-  if (cap < 0 || (cap > 0 && !out)) return HYDRA_ERR_INVALID;
-  std::map<std::string, hydra_kernel_stat_t> agg;
-  int status = HYDRA_OK;
-  for (ProfRec& r : g_prof) {
-    float ms = 0.f;
-    if (hipEventSynchronize(r.stop) != hipSuccess || hipEventElapsedTime(&ms, r.start, r.stop) != hipSuccess) {
-      status = HYDRA_ERR_HIP;
-      continue;
+  try {
+    std::lock_guard<std::mutex> lock(g_prof_mu);
+    g_prof_on = false;
+    if (cap < 0 || (cap > 0 && !out)) return HYDRA_ERR_INVALID;
+    std::map<std::string, hydra_kernel_stat_t> agg;
+    int status = HYDRA_OK;
+    for (ProfRec& r : g_prof) {
+      float ms = 0.f;
+      if (hipEventSynchronize(r.stop) != hipSuccess || hipEventElapsedTime(&ms, r.start, r.stop) != hipSuccess) {
+        status = HYDRA_ERR_HIP;
+        continue;
+      }
+      hydra_kernel_stat_t& k = agg[r.name];
+      if (k.launches == 0) {
+        std::memset(&k, 0, sizeof(k));
+        std::strncpy(k.name, r.name, sizeof(k.name) - 1);
+        k.min_ms = ms;
+        k.max_ms = ms;
+      }
+      k.launches += 1;
+      k.total_ms += ms;
+      k.min_ms = std::min<double>(k.min_ms, ms);
+      k.max_ms = std::max<double>(k.max_ms, ms);
     }
-    hydra_kernel_stat_t& k = agg[r.name];
-    if (k.launches == 0) {
-      std::memset(&k, 0, sizeof(k));
-      std::strncpy(k.name, r.name, sizeof(k.name) - 1);
-      k.min_ms = ms;
-      k.max_ms = ms;
+    prof_clear_locked();
+    if (status != HYDRA_OK) return status;
+    int n = 0;
+    for (auto& kv : agg) {
+      if (n < cap) out[n] = kv.second;
+      ++n;
     }
-    k.launches += 1;
-    k.total_ms += ms;
-    k.min_ms = std::min<double>(k.min_ms, ms);
-    k.max_ms = std::max<double>(k.max_ms, ms);
+    return n;
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
   }
-  prof_clear_locked();
-  if (status != HYDRA_OK) return status;
-  int n = 0;
-  for (auto& kv : agg) {
-    if (n < cap) out[n] = kv.second;
-    ++n;
-  }
-  return n;
 }
 
 void hydra_tile_rows(int32_t* q_tile_rows, int32_t* kv_tile_rows) {
