@@ -12,7 +12,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2609_34318_amd import hydra, ring
+from paper_2609_34318_amd import hydra, placement, ring
 
 from test_gpu_scores import BF16, MODS, Setup, _check_forward, _check_grads
 
@@ -169,3 +169,109 @@ def test_scores_are_as_near_as_stated(columns, cap, scale, size, biased):
     lse, A, s, B = _key_scores(q.to(BF16), k.to(BF16), scale, cap, slopes)
     allowed = 2.0 ** -21 * (np.abs(s) + B) + (2.0 ** -19 * np.abs(s) if cap else 0) + (2.0 ** -16 * A if columns > 1 else 0)
     assert (np.abs(lse - (s - B)) <= allowed).all()
+
+
+# ------------------------------------------------------------------ what the other tests leave out
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("cap", [2.0 ** -10, 2.0 ** 10])
+def test_caps_at_the_ends_of_their_range(cap, sign):
+    """Scores far beyond the cap, and scores around it, at the smallest and the largest cap."""
+    n = 130
+    s = Setup(([n], 2, 1, [(0, n)], [[(0, n)]]), "cap", seed=19)
+    s.cap, s.scores = cap, hydra.Scores(cap)
+    s.q.copy_((s.q.float() * sign * cap).to(BF16))  # scores of deviation one cap
+    O, L, rq, rkv = s.reference()
+    sh = s.share()
+    ring.forward(sh, s.q, s.kv)
+    vmax = float(s.kv[0][1].float().abs().max())
+    # weights are as far off as the scores: 2^-16 A of |q| |k| / sqrt(192) at most some 12 caps, 2^-19 of a cap; the sums of
+    # weights and values besides
+    off = 12 * 2.0 ** -16 * cap + 2.0 ** -18 * cap
+    assert np.abs(sh.o_acc.cpu().numpy() - O).max() <= (1.1 * 2.0 ** -8 + 2 * off) * vmax
+    assert np.abs(sh.lse_acc.cpu().numpy() - L).max() <= off + 2.0 ** -20 * np.abs(L).max()
+    dq, dkv = s.grads()
+    ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+    torch.cuda.synchronize()
+    if cap < 1:  # at the largest, one key takes a row's whole weight, and the gradients are roundings
+        _check_grads((dq, dkv), (rq, rkv), cap)
+    s.q.fill_(300.0 * sign)
+    s.kv[0][0].fill_(300.0)
+    ring.forward(sh, s.q, s.kv)
+    torch.cuda.synchronize()
+    want = cap * sign + np.log(np.arange(1, n + 1))
+    assert np.abs(sh.lse_acc.cpu().numpy()[0] - want).max() <= 2.0 ** -20 * (cap + 8)
+
+
+@pytest.mark.parametrize("case", ["tile_ends", "odd", "aligned_gqa"])
+def test_plain_gradients_against_this_oracle(case):
+    """The library's plain backward against the modified scores' oracle with nothing on."""
+    s = Setup(case, "prefix", seed=23)
+    s.prefix = None
+    O, L, rq, rkv = s.reference()
+    sh = s.share(scores=False)
+    ring.forward(sh, s.q, s.kv)
+    _check_forward(s, sh, O, L, "plain")
+    dq, dkv = s.grads()
+    ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+    torch.cuda.synchronize()
+    # D from the bf16 O, P to bf16 ahead of dS: two roundings more than the modified scores' kernels have
+    for name, x, y in [("dQ", dq, rq)] + [(n, a, b) for p, r in zip(dkv, rkv) for n, a, b in zip(("dK", "dV"), p, r)]:
+        x = x.double().cpu().numpy()
+        assert np.linalg.norm(x - y) <= 4 * 2.0 ** -8 * np.linalg.norm(y) + 2.0 ** -18 * math.sqrt(x.size), name
+
+
+def test_shares_of_scheduled_ranks():
+    """Every rank of a batch that is split over heads (two to four ranks) and over a ring, with the model's slopes, a cap
+    and the batch's prefixes: each rank's outputs are those of the unsplit documents' rows and heads."""
+    lens, H, cap, prefix = [900, 300, 40, 17], 4, 20.0, [200, 300, 0, 5]
+    mb, st, sz, _ = hydra.schedule(lens, 8, 160, pp=1)
+    slopes = torch.tensor([0.25, 0.0, 0.002, -0.001], device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(29)
+    docs = [[torch.randn((n, H, d), generator=g, device="cuda") for d in (192, 192, 128, 128)] for n in lens]
+    heads_seen = set()
+    for m in range(int(mb.max()) + 1):
+        for r in range(8):
+            share = placement.rank_share(lens, mb, st, sz, m, r, H)
+            if share is None:
+                continue
+            hs = slice(share.head0, share.head0 + share.n_heads)
+            heads_seen.add((share.head0, share.n_heads))
+            probs = placement.problems(share, softcap=cap, slopes=slopes, prefix=prefix)
+            for part, ps in zip(share.parts, probs):
+                window = [torch.cat([docs[i][t] for i in part.seqs])[:, hs] for t in range(4)]
+                rows = lambda segs: torch.cat([torch.arange(a, a + n) for a, n in segs])  # noqa: E731
+                s = Setup((np.diff(part.cu).tolist(), share.n_heads, share.n_kv_heads, part.q_segs, part.kv_steps), "cap")
+                s.cap, s.slopes, s.prefix, s.scores = cap, slopes[hs], [prefix[i] for i in part.seqs], ps[0].scores
+                at = rows(part.q_segs)
+                s.q, s.do = (window[t][at].to(BF16) for t in (0, 3))
+                s.kv = [tuple(window[t][rows(step)].to(BF16) for t in (1, 2)) for step in part.kv_steps]
+                O, L, rq, rkv = s.reference()
+                sh = s.share()
+                for p, q in zip(sh.problems, ps):
+                    assert hydra.workspace_size(p) == hydra.workspace_size(q) and hydra.visible_pairs(p) == hydra.visible_pairs(q)
+                sh.problems = ps
+                ring.forward(sh, s.q, s.kv)
+                _check_forward(s, sh, O, L, (m, r))
+                dq, dkv = s.grads()
+                ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+                torch.cuda.synchronize()
+                _check_grads((dq, dkv), (rq, rkv), (m, r))
+    assert {(h, 1) for h in range(H)} <= heads_seen and (2, 2) in heads_seen
+
+
+def test_timed_launches_carry_their_names():
+    s = Setup("aligned_gqa", "cap")
+    sh, stored = s.share(), s.share(True)
+    rope = hydra.Rope()
+    pos = torch.arange(s.nq, dtype=torch.int32, device="cuda")
+    hydra.profile_start()
+    ring.forward(sh, s.q, s.kv)
+    for x in (sh, stored):
+        dq, dkv = s.grads()
+        ring.backward(x, s.q, s.kv, s.do, dq, dkv) if x is sh else hydra.attn_bwd_ds(
+            x.problems[0], s.q, *s.kv[0], sh.o_acc, sh.lse_acc, s.do, dq, *dkv[0], x.ds_buf, x.workspace)
+    hydra.rope_q(rope, s.q, pos, torch.empty_like(s.q))
+    names = set(hydra.profile_stop())
+    assert {"attn_fwd_scores", "bwd_pre", "bwd_recompute_scores", "bwd_dkdv_ds_scores", "bwd_dq_ds_scores", "rope_q"} <= names
+    assert hydra.profile_stop() == {}
