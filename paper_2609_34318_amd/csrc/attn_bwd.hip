@@ -237,9 +237,8 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
         for (int e = 0; e < 16; ++e) {
           const int r = base + 16 * (e >> 3) + (e & 7);
           const bool vis = (unsigned)r < (unsigned)lim;
-          // a masked pair's tanh may be NaN, and with it the factor in dpd
-          if constexpr (MOD & kCap) ds[e] = vis ? __builtin_amdgcn_exp2f(arg(e)) * dpd(e) : 0.f;
-          else ds[e] = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY) * dpd(e);
+          const float p = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY);
+          ds[e] = (MOD & kCap) ? mul_zero(p, dpd(e)) : p * dpd(e);
         }
       }
       const bf16x8 dsf[2] = {to_bf16x8(ds), to_bf16x8(ds + 8)};
@@ -501,7 +500,6 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
                 const int r = base + 16 * (e >> 3) + (e & 7);
                 const bool vis = (unsigned)r < (unsigned)lim;
                 p[e] = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY);
-                if constexpr (MOD & kCap) f[e] = vis ? f[e] : 0.f;  // of a masked pair's tanh, which may be NaN
               }
             }
             pk[2 * sb] = to_bf16x8(p);
@@ -509,7 +507,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
             if constexpr (MOD != kPlain) {
 #pragma unroll
               for (int e = 0; e < 16; ++e)
-                if constexpr (MOD & kCap) p[e] *= f[e];
+                if constexpr (MOD & kCap) p[e] = mul_zero(p[e], f[e]);
               lds_st16<2048 * sb>(pbuf, poff, to_f16x8(p));
               lds_st16<2048 * sb + 1024>(pbuf, poff, to_f16x8(p + 8));
             } else {
