@@ -288,9 +288,11 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 // buffer descriptor is built per tile with its base at the tile's first row and its record
 // count ending at the tile's last valid row, so rows past the end are out of range for the
 // hardware bounds check and never touch memory (all of the offset travels in the VGPR
-// operand, which is what the check covers) (the kernels mask those rows and clear them in
-// LDS, clear_tail).  Each copy instruction
-// writes 16 (or 4) bytes per lane at LDS address M0 + 16*lane (4*lane).
+// operand, which is what the check covers).  For those rows gfx950 writes zeros to LDS (read back
+// for record counts inside a wave's copy, 16 and 4 bytes a lane).  No result is wrong without that:
+// the kernels mask the rows, and clear in LDS those that enter a product (clear_tail); but a cap's
+// choice of polynomial (cap_blocks) sees them, so that the last bits are the same in every run.  Each
+// copy instruction writes 16 (or 4) bytes per lane at LDS address M0 + 16*lane (4*lane).
 __device__ __forceinline__ u32x4 tile_desc(const void* base, int64_t byte_off, int bytes) {
   const uint64_t b = (uint64_t)(uintptr_t)base + (uint64_t)byte_off;
   u32x4 d;
@@ -373,8 +375,8 @@ __device__ __forceinline__ void dma_tile(lds_char* lds, u32x4 desc, int voff, in
 // Loading the fragments straight from global memory costs far more: each instruction then
 // touches 32 rows, and the 96 of a workgroup took about 6000 cycles.  The 16-byte chunk c of a
 // row's 64-column block lies at chunk c ^ (row & 7), which spreads both the copy and the reads
-// over the banks.  buf: OWN_BYTES<DIM> of LDS that only this wave uses.  Rows past `valid`
-// stay as they were in LDS: the caller masks them or does not store them.
+// over the banks.  buf: OWN_BYTES<DIM> of LDS that only this wave uses.  The caller masks rows past
+// `valid` or does not store them.
 template <int DIM> constexpr int own_bytes() { return 32 * DIM * 2; }
 template <int DIM>
 __device__ __forceinline__ void own_rows_issue(lds_char* buf, const uint16_t* g, int64_t row0, int valid, int pitch,
