@@ -135,9 +135,10 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   const float slope = slope_log2<MOD>(a, head);
   settle(lse2);
   settle(neg_D);
-  // With a cap the kernel needs some 14 registers more than it has: four of Q's fragments then stay in
-  // LDS behind the stages (spilled, their reloads also waited for the tile copies: 16K rows x 8 heads, recompute
-  // backward: 2682 us, spilled 2871; 2400 with fewer instructions around them)
+  // With a cap the kernel needs more registers than it has: four of Q's fragments then stay in LDS behind the
+  // stages.  With slopes too six registers would be spilled, whose reloads also wait for the tile copies (16K rows x
+  // 8 heads, recompute backward: 2301 us, spilled 2377); without slopes only two, and that form is 1% faster (2378
+  // and 2357)
   constexpr int Q_LDS = (MOD & kCap) ? 4 : 0, Q_REG = DQK / 16 - Q_LDS;
   static_assert(DQ_NSTAGE * DQ_STAGE + DQ_WAVES * Q_LDS * 1024 <= DQ_LDS, "LDS");
   lds_char* q_lds = smem + DQ_NSTAGE * DQ_STAGE + wave * (Q_LDS * 1024);

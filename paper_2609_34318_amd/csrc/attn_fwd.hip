@@ -33,7 +33,7 @@ constexpr float RESCALE_SLACK = 8.0f;
 // With modified scores the maximum has no slack: a row's largest weight is then 1, which its rounding to bf16
 // leaves as it is, and where that weight is nearly all of the row so are O and the backward's D (logits of
 // deviation 4: O off by 4e-4 of its norm instead of 1.2e-3, dQ and dK, rounded to bf16, by 2.4e-3 instead of
-// 2.8e-3; 16K rows x 8 heads: prefixes 645 to 668 us, cap 800 to 830, slopes the same).
+// 2.8e-3; 16K rows x 8 heads: prefixes 636 to 666 us, cap 751 to 773, slopes the same).
 template <int MOD> constexpr float slack() { return MOD == kPlain ? RESCALE_SLACK : 0.f; }
 
 // Starts the copy of key/value tile k into LDS stage `stage`.

@@ -60,10 +60,10 @@ template <int MOD> __device__ __forceinline__ float log2_unit(const Args<MOD>& a
 
 // out * tanh(s * scale / cap) of raw scores s: out is cap * log2(e) in the forward, whose scores are then in log2
 // units, and 1 in the backward, which needs 1 - tanh^2 and has a multiply-add for the exponent (16K rows x 8 heads,
-// recompute backward: in log2 units there too 2467 us, so 2436).  tanh(x) / x is a polynomial in x^2 of least
+// recompute backward: in log2 units there too 1.3% slower).  tanh(x) / x is a polynomial in x^2 of least
 // relative error, with the caps and the scale in its coefficients: of three (4e-7) up to |s| = small (TANH_SMALL
 // caps), of five (6e-7) up to |s| = near (TANH_NEAR caps).  A cap is some ten times the scores it is for, so most
-// blocks of 32 x 32 take the first (forward 823 us with the second alone, 779 with both; dK/dV 1611 and 1551), and
+// blocks of 32 x 32 take the first (forward 840 us with the second alone, 773 with both; dK/dV 1623 and 1533), and
 // few the exponential form beyond near, two quarter-rate instructions an element: tanh |x| =
 // 1 - 2 / (e^(2 |x|) + 1), of full relative accuracy there; infinite scores give the cap.  Four elements at a time,
 // whose chains of dependent instructions fill each other's latency.
