@@ -61,6 +61,27 @@ def test_gradients_beside_masked_scores_that_overflow(which, mod, ds):
     _check_grads((dq, dkv), (rq, rkv), which)
 
 
+@pytest.mark.parametrize("ds", [False, True])
+def test_visible_scores_that_overflow(ds):
+    """Products of finite values that are infinite: the scores are at the cap, of either sign, and do not move."""
+    n = 96
+    s = Setup(([n], 2, 1, [(0, n)], [[(0, n)]]), "cap")
+    s.cap, s.scores = 5.0, hydra.Scores(5.0)
+    up = torch.arange(n, device="cuda") % 3 != 0  # queries of one sign, keys of both
+    s.q.fill_(1e30)
+    s.kv[0][0].copy_(torch.where(up, 1e30, -1e30)[:, None, None].to(BF16).expand(n, 1, 192))
+    sh = s.share(ds)
+    assert (sh.ds_buf is not None) == ds
+    ring.forward(sh, s.q, s.kv)
+    score = np.where(up.cpu().numpy(), 5.0, -5.0)
+    want = np.array([np.logaddexp.reduce(score[:i + 1]) for i in range(n)])
+    assert np.abs(sh.lse_acc.cpu().numpy() - want).max() <= 2.0 ** -18 * 10
+    dq, dkv = s.grads()
+    ring.backward(sh, s.q, s.kv, s.do, dq, dkv)
+    torch.cuda.synchronize()
+    assert not dq.any() and not dkv[0][0].any() and bool(torch.isfinite(dkv[0][1]).all())
+
+
 def _poison(value):
     """Forward and both backwards over 512 rows x 256 heads of `value`, more workgroups than CUs."""
     n, H = 512, 256
