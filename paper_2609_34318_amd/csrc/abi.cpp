@@ -13,6 +13,7 @@
 #include "hydra_scores.h"
 #include "kernels.h"
 #include "plan.h"
+#include "plans.h"
 #include "prof.h"
 
 namespace hydra {
@@ -202,6 +203,25 @@ bool plan_matches(const void* ws, const Problem& pr, bool need_kitems, PlanRecor
   out->kv = it->second.kv;
   return true;
 }
+
+}  // namespace
+
+namespace hydra {
+// Plans of other kinds of calls, in the same map: an upload of either kind replaces what a workspace held.
+void plans_record(const void* ws, std::vector<int64_t>&& key) {
+  PlanRecord rec;
+  rec.key = std::move(key);
+  std::lock_guard<std::mutex> lock(g_plans_mu);
+  g_plans[ws] = std::move(rec);
+}
+bool plans_hold(const void* ws, const std::vector<int64_t>& key) {
+  std::lock_guard<std::mutex> lock(g_plans_mu);
+  auto it = g_plans.find(ws);
+  return it != g_plans.end() && it->second.key == key;
+}
+}  // namespace hydra
+
+namespace {
 
 AttnArgs base_args(const Problem& pr, const WsLayout& w, void* ws) {
   AttnArgs a{};

@@ -319,8 +319,10 @@ __device__ __forceinline__ u32x4 tile_rsrc(const uint16_t* g, int64_t row0, int 
   "s_add_u32 m0, m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen offset:%c" off " " hint "lds\n\t"
 template <int N, int STEP, int LSTEP, bool STREAM = false>
 __device__ __forceinline__ void dma_cols(uint32_t m0v, u32x4 desc, int voff) {
-  static_assert((N == 2 || N == 3) && (N - 1) * STEP < 4096, "immediate offsets");
-  if constexpr (N == 3)
+  static_assert(N >= 1 && N <= 3 && (N - 1) * STEP < 4096, "immediate offsets");
+  if constexpr (N == 1)
+    asm volatile(HYDRA_DMA_FIRST("") : : "v"(voff), "s"(m0v), "s"(desc) : "memory", "m0");
+  else if constexpr (N == 3)
     asm volatile(HYDRA_DMA_FIRST("") HYDRA_DMA_NEXT("4", "") HYDRA_DMA_NEXT("5", "")
                  :
                  : "v"(voff), "s"(m0v), "s"(desc), "n"(LSTEP - STEP), "n"(STEP), "n"(2 * STEP)

@@ -1,0 +1,741 @@
+// Linear attention with a decay for each head (hydra_linear.h).
+//
+// Every output is one recurrence with the operands changed about.  Over the rows of a sequence, in order or from the
+// last to the first,
+//   y_i = tx sum over j up to i of L^|i - j| <a_i, b_j> c_j  +  ts (decay since the chunk's edge) a_i S,
+// where S collects tu b_j^T c_j, decayed, over the rows before the chunk of i:
+//   forward   a, b, c = q, k, v              in order      tx = ts = scale, tu = 1
+//   dq        a, b, c = dO, v, k (S^T)       in order      the same
+//   dk        a, b, c = v, dO, q (G^T)       from the end  tx = tu = scale, ts = 1
+//   dv        a, b, c = k, q, dO (G)         from the end  the same
+// A workgroup walks the rows of one item (linear_plan.h) and head in chunks of 32; wave w holds the columns
+// 32 w .. 32 w + 31 of S in its accumulators, [d of a] x 32 in 32 bits, through the whole walk.  Per chunk it computes
+//   X = b a^T (32 x 32, every wave for itself: sharing it would take an exchange and a barrier), weighted by the decays,
+//   y^T = S^T a^T, weighted, + c^T X,
+//   S = L^32 S + b^T (weighted c).
+// The MFMA result layout is chosen (rows in the order pi, kernels.h) so that X, and S itself, are operands of the next
+// products as they lie in the registers; a, b and c come through swizzled LDS tiles, b and c by transpose reads too.
+// The next chunk's tiles are copied while one is computed.
+//
+// Sequences longer than an item are cut: a first launch (MAIN = false) leaves what each item adds to the state, a scan
+// turns that into the states that the items start from, and the main launch walks every item from its own.
+//
+// Rounding: MFMA operands are bf16.  X and S enter their products as sums of two bf16 values (16 bits), a weighted c as
+// a sum of two, or three (24 bits) where the walk ends in a state that the caller gets.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <initializer_list>
+
+#include "kernels.h"
+#include "linear_plan.h"
+#include "plans.h"
+#include "prof.h"
+
+namespace hydra {
+namespace {
+
+constexpr int LB = 32;  // rows of a chunk
+
+// One walk.  x_g: query heads per head of tensor x; x_s: elements between its token rows.
+struct Walk {
+  const uint16_t *a, *b, *c;
+  int a_s, b_s, c_s, a_g, b_g, c_g;
+  const float* in;   // the caller's states that sequences start from, or null
+  float* out;        // where their last states go, or null
+  float* slots;      // states of cut sequences' items
+  int trans;         // the caller's states are [columns of c][columns of a]
+  uint16_t* y;       // bf16 [rows][H][columns of c], or
+  float* y32;        // fp32; neither: only the last states
+  float tx, ts, tu;
+};
+struct Common {
+  const int* items;
+  const float* decay;
+  int n_items, H;
+};
+
+// exp2 arguments are multiples of this: finite, so that no decay times 0 rows is NaN
+__device__ __forceinline__ float log2_decay(const float* decay, int head) {
+  return fmax2(__int_as_float(((cint*)decay)[head]) * LOG2E, -1.0e30f);
+}
+
+// x as bf16, and what that leaves of it
+__device__ __forceinline__ void split_bf16(const float (&x)[8], bf16x8& hi, float (&rest)[8]) {
+  hi = to_bf16x8(x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = x[e] - (float)hi[e];
+}
+
+template <int DA, int DC, bool MAIN> struct LinGeom {
+  static constexpr int WAVES = DC / 32, COPY = WAVES >= 4 ? 4 : 2;  // waves that issue copies
+  static constexpr int A = MAIN ? LB * DA * 2 : 0, B = LB * DA * 2, C = LB * DC * 2, STAGE = A + B + C;
+  static constexpr int LDS = 2 * STAGE;
+};
+
+// The lane's part of a 32-column state [DA][32] in the caller's layout.
+template <int DA, int DC, class F> __device__ __forceinline__ void each_state(float* p, int trans, int wave, int lane, F&& f) {
+  const int m = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < DA / 32; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int da = 32 * b + 16 * (r >> 3) + 8 * h + (r & 7), dc = 32 * wave + m;
+      f(b, r, p + (trans ? dc * DA + da : da * DC + dc));
+    }
+}
+
+template <int DA, int DC, bool REV, bool MAIN>
+__device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int item, int head, lds_char* smem) {
+  typedef LinGeom<DA, DC, MAIN> G;
+  constexpr int NB = DA / 32;
+  const int tid = threadIdx.x, lane = tid & 63, m = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (wave >= G::WAVES) return;  // the launch has a wider walk too; ended waves are not waited for at barriers
+  const int* it = cm.items + (int64_t)item * LIN_INTS;
+  const int row0 = __builtin_amdgcn_readfirstlane(it[LIN_ROW0]), rows = __builtin_amdgcn_readfirstlane(it[LIN_ROWS]);
+  const int seq = __builtin_amdgcn_readfirstlane(it[LIN_SEQ]), slot = __builtin_amdgcn_readfirstlane(it[LIN_SLOT]);
+  const bool first = __builtin_amdgcn_readfirstlane(it[REV ? LIN_LAST : LIN_FIRST]) != 0;
+  const bool last = __builtin_amdgcn_readfirstlane(it[REV ? LIN_FIRST : LIN_LAST]) != 0;
+  if (!MAIN && (slot < 0 || last)) return;
+  const bool want_y = MAIN && (w.y || w.y32);
+  if (MAIN && !want_y && !(last && w.out)) return;
+
+  const float g2 = log2_decay(cm.decay, head);
+  auto power = [&](float e) { return __builtin_amdgcn_exp2f(g2 * e); };
+  const int n_chunks = (rows + LB - 1) / LB;
+  const int a_off = MAIN ? dma_lane_off<DA>(w.a_s, head / w.a_g, wave, lane) : 0;
+  const int b_off = dma_lane_off<DA>(w.b_s, head / w.b_g, wave, lane);
+  const int c_off = dma_lane_off<DC>(w.c_s, head / w.c_g, wave, lane);
+  auto chunk_row = [&](int t) { return LB * (REV ? n_chunks - 1 - t : t); };  // of the item
+  auto issue = [&](int t) {
+    if (wave >= G::COPY) return;
+    const int r = chunk_row(t), n = min(LB, rows - r);
+    const int64_t row = row0 + r;
+    lds_char* s = smem + (t & 1) * G::STAGE;
+    if constexpr (MAIN) dma_tile<DA, LB, G::COPY>(s, tile_rsrc(w.a, row, n, w.a_s), a_off, w.a_s, wave);
+    dma_tile<DA, LB, G::COPY>(s + G::A, tile_rsrc(w.b, row, n, w.b_s), b_off, w.b_s, wave);
+    dma_tile<DC, LB, G::COPY>(s + G::A + G::B, tile_rsrc(w.c, row, n, w.c_s), c_off, w.c_s, wave);
+  };
+
+  // the state that the item starts from
+  auto slot_at = [&](int s) {
+    return (char*)(w.slots + ((int64_t)s * cm.H + head) * (DA * DC)) + wave * (DA * 128) + lane * 16;
+  };
+  const int64_t user = ((int64_t)seq * cm.H + head) * (DA * DC);
+  f32x16 S[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) S[b] = f32x16{};
+  if (MAIN && slot >= 0) {
+    const char* p = slot_at(slot);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p + (4 * b + rr) * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[b][4 * rr + e] = v[e];
+      }
+  } else if (first && w.in) {
+    each_state<DA, DC>(const_cast<float*>(w.in) + user, w.trans, wave, lane, [&](int b, int r, float* p) { S[b][r] = *p; });
+  }
+  auto store_slot = [&](int s) {
+    char* p = slot_at(s);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        *reinterpret_cast<f32x4*>(p + (4 * b + rr) * 1024) =
+            f32x4{S[b][4 * rr], S[b][4 * rr + 1], S[b][4 * rr + 2], S[b][4 * rr + 3]};
+  };
+  // the main launch's first item takes its start from a slot too: the caller's last states may replace the first
+  if (!MAIN && first) store_slot(slot);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) settle(S[b]);
+
+  // weights: of X at this lane's element r, of the row of y, of c at this lane's rows
+  float wx[16], wu[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int j = 16 * (r >> 3) + 8 * h + (r & 7), d = REV ? j - m : m - j;
+    wx[r] = d < 0 ? 0.f : w.tx * power(float(d));
+    wu[r] = w.tu * power(float(REV ? j + 1 : LB - 1 - j));
+  }
+  const float full_decay = power(float(LB));
+  const bool three = w.out != nullptr;  // uniform
+
+  OperandOffsets o = operand_offsets(lane);
+  int nat[4];  // as o.b128, of row m
+#pragma unroll
+  for (int j = 0; j < 4; ++j) nat[j] = m * 128 + (((2 * j + h) ^ swz(m)) << 4);
+  int trp[2][2];  // as o.tr, columns in the order pi
+  {
+    const int g = lane >> 4, gi = lane & 15, x = gi & 3, sw = ((x & 1) << 1) | (x >> 1);
+    const int cl = 2 * (g & 1) + (sw >> 1), half = (sw & 1) << 3;
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int r = 8 * h + (gi >> 2) + 4 * v;
+        trp[v][k] = r * 128 + (((4 * k + cl) ^ swz(r)) << 4) + half;
+      }
+  }
+  // transpose reads of the wave's own columns of c
+  const int ct0 = (wave >> 1) * block_bytes<LB>() + ((wave & 1) ? o.tr[0][1] : o.tr[0][0]);
+  const int ct1 = (wave >> 1) * block_bytes<LB>() + ((wave & 1) ? o.tr[1][1] : o.tr[1][0]);
+
+  if (n_chunks > 0) issue(0);
+  for (int t = 0; t < n_chunks; ++t) {
+    const int r0 = chunk_row(t), n = min(LB, rows - r0);
+    lds_char* As = smem + (t & 1) * G::STAGE;
+    lds_char* Bs = As + G::A;
+    lds_char* Cs = Bs + G::B;
+    // this chunk's copies; the stores of the last one's rows, issued behind them, may be in flight
+    if (t == 0 || !want_y) wait_dma();
+    else if (w.y) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    if (n < LB && wave < G::COPY) {
+      clear_tail<DA, LB, G::COPY>(Bs, n, wave, lane);
+      clear_tail<DC, LB, G::COPY>(Cs, n, wave, lane);
+    }
+    barrier_lds();
+    if (t + 1 < n_chunks) issue(t + 1);
+
+    bf16x8 cf[2];  // c^T: lane = column, rows 16 s + 8 h .. + 7
+#pragma unroll
+    for (int s = 0; s < 2; ++s) cf[s] = join(lds_tr8(Cs + 2048 * s + ct0), lds_tr8(Cs + 2048 * s + ct1));
+
+    if (want_y) {
+      f32x16 x = f32x16{}, y = f32x16{};
+#pragma unroll
+      for (int k = 0; k < DA / 16; ++k) {
+        const bf16x8 af = lds_ld16(As, nat[k & 3] + (k >> 2) * block_bytes<LB>());
+        x = mfma(op_b128<LB>(Bs, o, 0, k), af, x);
+        float s8[8], rest[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s8[e] = S[k >> 1][8 * (k & 1) + e];
+        bf16x8 hi;
+        split_bf16(s8, hi, rest);
+        y = mfma(hi, af, y);
+        y = mfma(to_bf16x8(rest), af, y);
+      }
+      y *= w.ts * power(float(REV ? n - 1 - m : m + 1));
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        float p[8], rest[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = x[8 * s + e] * wx[8 * s + e];
+        bf16x8 hi;
+        split_bf16(p, hi, rest);
+        y = mfma(cf[s], hi, y);
+        y = mfma(cf[s], to_bf16x8(rest), y);
+      }
+      // rows out through c's tile, which every wave has read
+      barrier_lds();
+      const int pitch = cm.H * DC;
+      const int64_t at = ((int64_t)(row0 + r0) * cm.H + head) * DC;
+      if (w.y) {
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr)
+          *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(Cs + m * (DC * 2) + (((4 * wave + rr) ^ (m & 7)) << 4) + 8 * h) =
+              u32x2{pack_bf16x2(y[4 * rr], y[4 * rr + 1]), pack_bf16x2(y[4 * rr + 2], y[4 * rr + 3])};
+        barrier_lds();
+        const rows_rsrc ry = rows_buffer(w.y + at, n, pitch * 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int idx = tid + 2 * DC * i, row = idx / (DC / 8), ch = idx % (DC / 8);
+          const u32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(Cs + row * (DC * 2) + ((ch ^ (row & 7)) << 4));
+          __builtin_amdgcn_raw_buffer_store_b128(v, ry, row * pitch * 2 + ch * 16, 0, 0);
+        }
+      } else {  // 32 bits: 16 rows at a time
+        const rows_rsrc ry = rows_buffer(w.y32 + at, n, pitch * 4);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if ((m >> 4) == half) {
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr)
+              *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(Cs + (m & 15) * (DC * 4) + (((8 * wave + 2 * rr + h) ^ (m & 7)) << 4)) =
+                  f32x4{y[4 * rr], y[4 * rr + 1], y[4 * rr + 2], y[4 * rr + 3]};
+          }
+          barrier_lds();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int idx = tid + 2 * DC * i, row = idx / (DC / 4), ch = idx % (DC / 4);
+            const u32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(Cs + row * (DC * 4) + ((ch ^ (row & 7)) << 4));
+            __builtin_amdgcn_raw_buffer_store_b128(v, ry, (16 * half + row) * pitch * 4 + ch * 16, 0, 0);
+          }
+          if (half == 0) barrier_lds();
+        }
+      }
+    }
+
+    // S = L^n S + b^T (weighted c)
+    const float dec = n == LB ? full_decay : power(float(n));
+#pragma unroll
+    for (int b = 0; b < NB; ++b) S[b] *= dec;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float c8[8], rest[8], rest2[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float u = wu[8 * s + e];
+        if (!REV && n < LB) u = w.tu * power(float(max(n - 1 - (16 * s + 8 * h + e), 0)));
+        c8[e] = (float)cf[s][e] * u;
+      }
+      bf16x8 part[3];
+      split_bf16(c8, part[0], rest);
+      split_bf16(rest, part[1], rest2);
+      part[2] = to_bf16x8(rest2);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const lds_char* q = Bs + (b >> 1) * block_bytes<LB>() + 2048 * s;
+        const bf16x8 bf = join(lds_tr8(q + trp[0][b & 1]), lds_tr8(q + trp[1][b & 1]));
+        S[b] = mfma(bf, part[0], S[b]);
+        S[b] = mfma(bf, part[1], S[b]);
+        if (three) S[b] = mfma(bf, part[2], S[b]);
+      }
+    }
+  }
+
+  if (!MAIN) store_slot(REV ? slot - 1 : slot + 1);
+  else if (last && w.out)
+    each_state<DA, DC>(w.out + user, w.trans, wave, lane, [&](int b, int r, float* p) { *p = S[b][r]; });
+}
+
+template <int DK, int DV, bool MAIN>
+__global__ __launch_bounds__(2 * DV) void lin_fwd_kernel(Walk w, Common cm) {
+  __shared__ __attribute__((aligned(1024))) char smem[LinGeom<DK, DV, MAIN>::LDS];
+  lin_walk<DK, DV, false, MAIN>(w, cm, blockIdx.x / cm.H, blockIdx.x % cm.H, (lds_char*)smem);
+}
+
+// The three walks of an item and head run on one XCD (workgroup b runs on XCD b % 8), one after another, and find each
+// other's tiles in its L2.
+template <int DK, int DV, bool MAIN>
+__global__ __launch_bounds__(2 * (DK > DV ? DK : DV)) void lin_bwd_kernel(Walk dq, Walk dk, Walk dv, Common cm) {
+  constexpr int L0 = LinGeom<DV, DK, MAIN>::LDS, L1 = LinGeom<DK, DV, MAIN>::LDS;
+  __shared__ __attribute__((aligned(1024))) char smem[L0 > L1 ? L0 : L1];
+  const int j = blockIdx.x / N_XCD, role = j % 3, unit = j / 3 * N_XCD + blockIdx.x % N_XCD;
+  const int item = unit / cm.H, head = unit % cm.H;
+  if (item >= cm.n_items) return;
+  if (role == 0) lin_walk<DV, DK, false, MAIN>(dq, cm, item, head, (lds_char*)smem);
+  else if (role == 1) lin_walk<DV, DK, true, MAIN>(dk, cm, item, head, (lds_char*)smem);
+  else lin_walk<DK, DV, true, MAIN>(dv, cm, item, head, (lds_char*)smem);
+}
+
+// The states that a cut sequence's items start from, out of what each adds: in order slot s = L^seg slot (s - 1) +
+// slot s from the third on (the first holds the start and the second the state behind the first item), from the end
+// the same backwards.  One lane walks four elements; eight slots' loads are in flight.
+struct Scan {
+  float* slots;
+  int rev;
+};
+__global__ __launch_bounds__(256) void lin_scan_kernel(Scan s0, Scan s1, Scan s2, const int* scans, Common cm, int seg, int dd) {
+  const Scan s = blockIdx.z == 0 ? s0 : blockIdx.z == 1 ? s1 : s2;
+  const int scan = blockIdx.y / cm.H, head = blockIdx.y % cm.H;
+  const int slot0 = scans[2 * scan], n = scans[2 * scan + 1];
+  const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= dd) return;
+  const float decay = __builtin_amdgcn_exp2f(log2_decay(cm.decay, head) * float(seg));
+  const int64_t step = (int64_t)cm.H * dd * (s.rev ? -1 : 1);
+  float* p = s.slots + ((int64_t)(s.rev ? slot0 + n - 1 : slot0) * cm.H + head) * dd + e;
+  f32x4 v = *reinterpret_cast<const f32x4*>(p + step);
+  constexpr int AHEAD = 8;
+  for (int i = 2; i < n; i += AHEAD) {
+    f32x4 u[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i + k < n) u[k] = *reinterpret_cast<const f32x4*>(p + (i + k) * step);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i + k < n) {
+        v = v * decay + u[k];
+        *reinterpret_cast<f32x4*>(p + (i + k) * step) = v;
+      }
+  }
+}
+
+// Sums over the query heads of a K/V head: x [rows][Hkv][grp][d] in 32 bits -> y [rows][Hkv][d] bf16.
+__global__ __launch_bounds__(256) void lin_group_kernel(const float* __restrict__ x, uint16_t* __restrict__ y, int64_t n8,
+                                                        int d8, int grp) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
+    const float* p = x + (i / d8 * grp * d8 + i % d8) * 8;
+    f32x4 lo = f32x4{}, hi = f32x4{};
+    for (int g = 0; g < grp; ++g, p += d8 * 8) {
+      lo += *reinterpret_cast<const f32x4*>(p);
+      hi += *reinterpret_cast<const f32x4*>(p + 4);
+    }
+    const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    *reinterpret_cast<bf16x8*>(y + i * 8) = to_bf16x8(v);
+  }
+}
+
+// ------------------------------------------------------------------ one token
+// A workgroup takes 32 columns of one row's and head's state: lane group r = tid / 8 its rows r, r + 16, ..., lane
+// tid % 8 four columns.  Bound by the state's bytes.  The first row of a slot takes the later ones too, in order, with
+// the state in its registers.
+constexpr int STEP_THREADS = 128;
+template <int DK, int DV>
+__global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int n_slots, int H, int Hkv, float scale,
+                                                                const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+                                                                const uint16_t* __restrict__ v, const float* __restrict__ decay,
+                                                                const float* state, float* state_out,
+                                                                const int* __restrict__ slots, uint16_t* __restrict__ o) {
+  constexpr int NR = DK / 16;
+  __shared__ f32x4 part[2][8];
+  __shared__ int next_row[2];
+  const int tid = threadIdx.x, r = tid >> 3, c4 = tid & 7;
+  const int cb = blockIdx.x % (DV / 32), rest = blockIdx.x / (DV / 32), head = rest % H;
+  int row = rest / H;
+  const int slot = slots ? slots[row] : row;
+  if (slot < 0 || slot >= n_slots) return;
+  const int kv = head / (H / Hkv);
+  const int64_t at = ((int64_t)slot * H + head) * (DK * DV) + (int64_t)r * DV + 32 * cb + 4 * c4;
+  f32x4 S[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) S[i] = *reinterpret_cast<const f32x4*>(state + at + i * 16 * DV);
+  if (slots) {  // not the slot's first row: nothing to do
+    int earlier = 0;
+    for (int b = tid; b < row; b += STEP_THREADS) earlier |= slots[b] == slot;
+    if (__syncthreads_or(earlier)) return;
+  }
+  const float dec = expf(fmax2(decay[head], -1.0e30f));
+  for (;;) {
+    const int64_t kq = ((int64_t)row * Hkv + kv) * DK, qq = ((int64_t)row * H + head) * DK;
+    const u32x2 vv = *reinterpret_cast<const u32x2*>(v + ((int64_t)row * Hkv + kv) * DV + 32 * cb + 4 * c4);
+    const f32x4 v4 = {__uint_as_float(vv[0] << 16), __uint_as_float(vv[0] & 0xffff0000u), __uint_as_float(vv[1] << 16),
+                      __uint_as_float(vv[1] & 0xffff0000u)};
+    f32x4 sum = f32x4{};
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const float ki = __uint_as_float((uint32_t)k[kq + r + 16 * i] << 16), qi = __uint_as_float((uint32_t)q[qq + r + 16 * i] << 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        S[i][e] = __builtin_fmaf(ki, v4[e], S[i][e] * dec);
+        sum[e] = __builtin_fmaf(qi, S[i][e], sum[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sum[e] += __shfl_xor(sum[e], 8, 64);
+      sum[e] += __shfl_xor(sum[e], 16, 64);
+      sum[e] += __shfl_xor(sum[e], 32, 64);
+    }
+    // the slot's next row
+    int next = 0x7fffffff;
+    if (slots)
+      for (int b = row + 1 + tid; b < n_rows; b += STEP_THREADS)
+        if (slots[b] == slot) {
+          next = b;
+          break;
+        }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) next = min(next, __shfl_xor(next, d, 64));
+    if ((tid & 63) < 8) part[tid >> 6][tid & 7] = sum;
+    if ((tid & 63) == 0) next_row[tid >> 6] = next;
+    __syncthreads();
+    if (tid < 8) {
+      const f32x4 t = (part[0][tid] + part[1][tid]) * scale;
+      *reinterpret_cast<u32x2*>(o + ((int64_t)row * H + head) * DV + 32 * cb + 4 * tid) =
+          u32x2{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+    }
+    next = min(next_row[0], next_row[1]);
+    if (next == 0x7fffffff) break;
+    row = next;
+    __syncthreads();  // part and next_row are read
+  }
+#pragma unroll
+  for (int i = 0; i < NR; ++i) *reinterpret_cast<f32x4*>(state_out + at + i * 16 * DV) = S[i];
+}
+
+// ------------------------------------------------------------------ host side
+
+// f with the head sizes as compile-time numbers.
+template <class F> hipError_t with_dims(int dk, int dv, F&& f) {
+  if (dv == 64)
+    return dk == 64 ? f(IntC<64>{}, IntC<64>{}) : dk == 128 ? f(IntC<128>{}, IntC<64>{}) : f(IntC<192>{}, IntC<64>{});
+  return dk == 64 ? f(IntC<64>{}, IntC<128>{}) : dk == 128 ? f(IntC<128>{}, IntC<128>{}) : f(IntC<192>{}, IntC<128>{});
+}
+
+struct Timed {
+  int tok;
+  hipStream_t s;
+  Timed(const char* name, hipStream_t st) : tok(prof_begin(name, st)), s(st) {}
+  ~Timed() { prof_end(tok, s); }
+};
+
+struct Span {
+  const void* p;
+  uint64_t n;
+};
+bool overlap(Span a, Span b) {
+  if (!a.p || !b.p || a.n == 0 || b.n == 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y + b.n && y < x + a.n;
+}
+bool outputs_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    for (auto o2 = o + 1; o2 != outs.end(); ++o2)
+      if (overlap(*o, *o2)) return true;
+    for (const Span& i : ins)
+      if (overlap(*o, i)) return true;
+  }
+  return false;
+}
+bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t width) {
+  return rows > 0 ? uint64_t((rows - 1) * stride + width) * 2 : 0;
+}
+
+// What a plan depends on; the leading number is no head count of an attention plan's.
+std::vector<int64_t> linear_key(const LinearProblem& pr) {
+  std::vector<int64_t> k = {-2, pr.H};
+  k.insert(k.end(), pr.cu.begin(), pr.cu.end());
+  return k;
+}
+
+int upload(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, void* ws, hipStream_t s) {
+  std::vector<int32_t> image(w.slots_off / sizeof(int32_t), 0);
+  std::copy(plan.items.begin(), plan.items.end(), image.begin() + int64_t(w.items_off / sizeof(int32_t)));
+  std::copy(plan.scans.begin(), plan.scans.end(), image.begin() + int64_t(w.scans_off / sizeof(int32_t)));
+  // pageable source: the runtime has consumed the image when the call returns
+  if (!image.empty() &&
+      hipMemcpyAsync(ws, image.data(), image.size() * sizeof(int32_t), hipMemcpyHostToDevice, s) != hipSuccess)
+    return HYDRA_ERR_HIP;
+  plans_record(ws, linear_key(pr));
+  return HYDRA_OK;
+}
+
+// The workspace checked and holding the plan.
+int ready(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, bool planned, void* ws, size_t bytes,
+          hipStream_t s) {
+  if (!planned) return upload(pr, plan, w, ws, s);
+  return plans_hold(ws, linear_key(pr)) ? HYDRA_OK : HYDRA_ERR_WORKSPACE;
+}
+
+hipError_t scan(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, char* ws, const Common& cm,
+                std::initializer_list<Scan> walks, hipStream_t s) {
+  const Scan* p = walks.begin();
+  const int n = int(walks.size()), dd = pr.dk * pr.dv;
+  Timed timed("linear_scan", s);
+  // a grid's second size ends at 65535
+  const int per = std::max(1, 65535 / pr.H);
+  for (int at = 0; at < plan.n_scans; at += per)
+    hipLaunchKernelGGL(lin_scan_kernel, dim3(unsigned(dd + 1023) / 1024, unsigned(std::min(per, plan.n_scans - at) * pr.H), unsigned(n)),
+                       dim3(256), 0, s, p[0], p[n > 1 ? 1 : 0], p[n > 2 ? 2 : 0],
+                       reinterpret_cast<const int*>(ws + w.scans_off) + 2 * at, cm, plan.seg, dd);
+  return hipGetLastError();
+}
+
+int linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
+               const float* state_in, void* o, float* state_out, void* workspace, size_t bytes, bool planned, void* stream) {
+  LinearProblem pr;
+  if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+  const uint64_t states = uint64_t(pr.cu.size() - 1) * pr.H * pr.dk * pr.dv * 4;
+  if (!decay) return HYDRA_ERR_INVALID;
+  if (pr.rows > 0 && (!q || !k || !v || (!o && !state_out))) return HYDRA_ERR_INVALID;
+  for (const void* x : {q, k, v, static_cast<const void*>(state_in), static_cast<const void*>(o), static_cast<const void*>(state_out)})
+    if (misaligned(x, 16)) return HYDRA_ERR_ALIGN;
+  if (misaligned(decay, 4)) return HYDRA_ERR_ALIGN;
+  LinearPlan plan;
+  linear_plan(pr, &plan);
+  const LinearLayout w = linear_layout(pr, plan);
+  if (!workspace || bytes < w.total) return HYDRA_ERR_WORKSPACE;
+  if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  const Span outs[3] = {{o, uint64_t(pr.rows) * pr.H * pr.dv * 2}, {state_out, states}, {workspace, w.total}};
+  const Span qs{q, rows_bytes(pr.rows, pr.q_s, pr.H * pr.dk)}, ks{k, rows_bytes(pr.rows, pr.k_s, pr.Hkv * pr.dk)},
+      vs{v, rows_bytes(pr.rows, pr.v_s, pr.Hkv * pr.dv)}, ds{decay, uint64_t(pr.H) * 4},
+      is{state_in == state_out ? nullptr : state_in, states}, is2{state_in, states};
+  if (outputs_overlap({outs[0], outs[1], outs[2]}, {qs, ks, vs, ds, is}) || overlap(outs[0], is2) || overlap(outs[2], is2))
+    return HYDRA_ERR_INVALID;
+  if (pr.rows == 0 && !state_out) return HYDRA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (int rc = ready(pr, plan, w, planned, workspace, bytes, s); rc != HYDRA_OK) return rc;
+  char* ws = static_cast<char*>(workspace);
+  const Common cm{reinterpret_cast<const int*>(ws + w.items_off), decay, plan.n_items, pr.H};
+  const int grp = pr.H / pr.Hkv;
+  auto u16 = [](const void* x) { return static_cast<const uint16_t*>(x); };
+  const Walk walk{u16(q), u16(k), u16(v), pr.q_s, pr.k_s, pr.v_s, 1, grp, grp, state_in, state_out,
+                  reinterpret_cast<float*>(ws + w.slots_off), 0, static_cast<uint16_t*>(o), nullptr, pr.scale, pr.scale, 1.f};
+  const hipError_t e = with_dims(pr.dk, pr.dv, [&](auto dk_, auto dv_) {
+    constexpr int DK = decltype(dk_)::value, DV = decltype(dv_)::value;
+    if (plan.n_split > 0) {
+      {
+        Timed timed("linear_states", s);
+        hipLaunchKernelGGL((lin_fwd_kernel<DK, DV, false>), dim3(unsigned(plan.n_split) * pr.H), dim3(2 * DV), 0, s, walk, cm);
+      }
+      if (hipError_t x = scan(pr, plan, w, ws, cm, {Scan{walk.slots, 0}}, s); x != hipSuccess) return x;
+    }
+    Timed timed("linear_fwd", s);
+    hipLaunchKernelGGL((lin_fwd_kernel<DK, DV, true>), dim3(unsigned(plan.n_items) * pr.H), dim3(2 * DV), 0, s, walk, cm);
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
+}
+
+int linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
+               const float* state_in, const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv,
+               float* d_state_in, void* workspace, size_t bytes, bool planned, void* stream) {
+  LinearProblem pr;
+  if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+  const uint64_t states = uint64_t(pr.cu.size() - 1) * pr.H * pr.dk * pr.dv * 4;
+  if (!decay) return HYDRA_ERR_INVALID;
+  if (pr.rows > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv)) return HYDRA_ERR_INVALID;
+  for (const void* x : {q, k, v, static_cast<const void*>(state_in), d_o, static_cast<const void*>(d_state_out),
+                        static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv),
+                        static_cast<const void*>(d_state_in)})
+    if (misaligned(x, 16)) return HYDRA_ERR_ALIGN;
+  if (misaligned(decay, 4)) return HYDRA_ERR_ALIGN;
+  LinearPlan plan;
+  linear_plan(pr, &plan);
+  const LinearLayout w = linear_layout(pr, plan);
+  if (!workspace || bytes < w.total) return HYDRA_ERR_WORKSPACE;
+  if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  const uint64_t n = uint64_t(pr.rows);
+  if (outputs_overlap({{dq, n * pr.H * pr.dk * 2}, {dk, n * pr.Hkv * pr.dk * 2}, {dv, n * pr.Hkv * pr.dv * 2},
+                       {d_state_in, states}, {workspace, w.total}},
+                      {{q, rows_bytes(pr.rows, pr.q_s, pr.H * pr.dk)}, {k, rows_bytes(pr.rows, pr.k_s, pr.Hkv * pr.dk)},
+                       {v, rows_bytes(pr.rows, pr.v_s, pr.Hkv * pr.dv)}, {decay, uint64_t(pr.H) * 4}, {state_in, states},
+                       {d_o, n * pr.H * pr.dv * 2}, {d_state_out, states}}))
+    return HYDRA_ERR_INVALID;
+  if (pr.rows == 0 && !d_state_in) return HYDRA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (int rc = ready(pr, plan, w, planned, workspace, bytes, s); rc != HYDRA_OK) return rc;
+  char* ws = static_cast<char*>(workspace);
+  const Common cm{reinterpret_cast<const int*>(ws + w.items_off), decay, plan.n_items, pr.H};
+  const int grp = pr.H / pr.Hkv, dos = pr.H * pr.dv;
+  const int64_t slots = int64_t(plan.n_split) * pr.H * pr.dk * pr.dv;
+  float* at = reinterpret_cast<float*>(ws + w.slots_off);
+  auto u16 = [](const void* x) { return static_cast<const uint16_t*>(x); };
+  auto out16 = [&](void* x) { return grp > 1 ? nullptr : static_cast<uint16_t*>(x); };
+  auto out32 = [&](size_t off) { return grp > 1 ? reinterpret_cast<float*>(ws + off) : nullptr; };
+  const Walk wq{u16(d_o), u16(v), u16(k), dos, pr.v_s, pr.k_s, 1, grp, grp, state_in, nullptr, at, 1,
+                static_cast<uint16_t*>(dq), nullptr, pr.scale, pr.scale, 1.f};
+  const Walk wk{u16(v), u16(d_o), u16(q), pr.v_s, dos, pr.q_s, grp, 1, 1, d_state_out, nullptr, at + slots, 1,
+                out16(dk), out32(w.dk_off), pr.scale, 1.f, pr.scale};
+  const Walk wv{u16(k), u16(q), u16(d_o), pr.k_s, pr.q_s, dos, grp, 1, 1, d_state_out, d_state_in, at + 2 * slots, 0,
+                out16(dv), out32(w.dv_off), pr.scale, 1.f, pr.scale};
+  const hipError_t e = with_dims(pr.dk, pr.dv, [&](auto dk_, auto dv_) {
+    constexpr int DK = decltype(dk_)::value, DV = decltype(dv_)::value;
+    auto grid = [&](int items) { return dim3(unsigned((int64_t(items) * pr.H + N_XCD - 1) / N_XCD * N_XCD * 3)); };
+    const dim3 block(2 * std::max(DK, DV));
+    if (plan.n_split > 0) {
+      {
+        Common first = cm;
+        first.n_items = plan.n_split;
+        Timed timed("linear_states", s);
+        hipLaunchKernelGGL((lin_bwd_kernel<DK, DV, false>), grid(plan.n_split), block, 0, s, wq, wk, wv, first);
+      }
+      if (hipError_t x = scan(pr, plan, w, ws, cm, {Scan{wq.slots, 0}, Scan{wk.slots, 1}, Scan{wv.slots, 1}}, s); x != hipSuccess)
+        return x;
+    }
+    {
+      Timed timed("linear_bwd", s);
+      hipLaunchKernelGGL((lin_bwd_kernel<DK, DV, true>), grid(plan.n_items), block, 0, s, wq, wk, wv, cm);
+    }
+    if (grp > 1 && pr.rows > 0) {
+      Timed timed("linear_groups", s);
+      auto sum = [&](const float* x, void* y, int d) {
+        const int64_t n8 = pr.rows * pr.Hkv * d / 8;
+        hipLaunchKernelGGL(lin_group_kernel, dim3(unsigned(std::min<int64_t>((n8 + 255) / 256, 1 << 16))), dim3(256), 0, s, x,
+                           static_cast<uint16_t*>(y), n8, d / 8, grp);
+      };
+      sum(wk.y32, dk, DK);
+      sum(wv.y32, dv, DV);
+    }
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace hydra
+
+using namespace hydra;
+
+extern "C" {
+
+size_t hydra_linear_workspace_size(const hydra_linear_t* p) {
+  try {
+    LinearProblem pr;
+    if (check_linear(p, &pr) != HYDRA_OK) return 0;
+    LinearPlan plan;
+    linear_plan(pr, &plan);
+    return linear_layout(pr, plan).total;
+  } catch (...) {
+    return 0;
+  }
+}
+
+int hydra_linear_plan(const hydra_linear_t* p, void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    LinearProblem pr;
+    if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+    LinearPlan plan;
+    linear_plan(pr, &plan);
+    const LinearLayout w = linear_layout(pr, plan);
+    if (!workspace || workspace_bytes < w.total) return HYDRA_ERR_WORKSPACE;
+    if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+    return upload(pr, plan, w, workspace, static_cast<hipStream_t>(stream));
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
+  }
+}
+
+int hydra_linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
+                     const float* state_in, void* o, float* state_out, void* workspace, size_t workspace_bytes,
+                     int32_t planned, void* stream) {
+  try {
+    return linear_fwd(p, q, k, v, decay, state_in, o, state_out, workspace, workspace_bytes, planned != 0, stream);
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
+  }
+}
+
+int hydra_linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
+                     const float* state_in, const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv,
+                     float* d_state_in, void* workspace, size_t workspace_bytes, int32_t planned, void* stream) {
+  try {
+    return linear_bwd(p, q, k, v, decay, state_in, d_o, d_state_out, dq, dk, dv, d_state_in, workspace, workspace_bytes,
+                      planned != 0, stream);
+  } catch (...) {
+    return HYDRA_ERR_INVALID;
+  }
+}
+
+int hydra_linear_step(int32_t n_rows, int32_t n_slots, int32_t n_heads, int32_t n_kv_heads, int32_t d_k, int32_t d_v,
+                      float scale, const void* q, const void* k, const void* v, const float* decay, const float* state,
+                      float* state_out, const int32_t* slots, void* o, void* stream) {
+  const int hkv = n_kv_heads == 0 ? n_heads : n_kv_heads;
+  if (n_rows < 0 || n_rows > 65536 || n_slots < 0 || n_heads <= 0 || n_heads > 4096) return HYDRA_ERR_INVALID;
+  if (hkv < 0 || hkv > n_heads || n_heads % hkv != 0 || d_k <= 0 || d_v <= 0) return HYDRA_ERR_INVALID;
+  if ((d_k != 64 && d_k != 128 && d_k != 192) || (d_v != 64 && d_v != 128)) return HYDRA_ERR_UNSUPPORTED;
+  if (!(scale - scale == 0.f)) return HYDRA_ERR_INVALID;  // not finite
+  if (!slots && n_slots < n_rows) return HYDRA_ERR_INVALID;
+  // a dispatch holds fewer than 2^32 lanes
+  if (int64_t(n_rows) * n_heads * (d_v / 32) >= (int64_t(1) << 32) / STEP_THREADS) return HYDRA_ERR_INVALID;
+  if (n_rows == 0) return HYDRA_OK;
+  if (!q || !k || !v || !decay || !state || !state_out || !o) return HYDRA_ERR_INVALID;
+  for (const void* x : {q, k, v, static_cast<const void*>(state), static_cast<const void*>(state_out), static_cast<const void*>(o)})
+    if (misaligned(x, 16)) return HYDRA_ERR_ALIGN;
+  if (misaligned(decay, 4) || misaligned(slots, 4)) return HYDRA_ERR_ALIGN;
+  const uint64_t n = uint64_t(n_rows), states = uint64_t(n_slots) * n_heads * d_k * d_v * 4;
+  const Span so{state_out, states}, si{state, states}, os{o, n * n_heads * d_v * 2};
+  if (outputs_overlap({os, so}, {{q, n * n_heads * d_k * 2}, {k, n * hkv * d_k * 2}, {v, n * hkv * d_v * 2},
+                                 {decay, uint64_t(n_heads) * 4}, {slots, n * 4}}) ||
+      overlap(os, si) || (state != state_out && overlap(so, si)))
+    return HYDRA_ERR_INVALID;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const float sc = scale > 0.f ? scale : 1.0f / sqrtf(float(d_k));
+  const hipError_t e = with_dims(d_k, d_v, [&](auto dk_, auto dv_) {
+    constexpr int DK = decltype(dk_)::value, DV = decltype(dv_)::value;
+    Timed timed("linear_step", s);
+    hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(unsigned(n_rows) * unsigned(n_heads) * (DV / 32)), dim3(STEP_THREADS), 0,
+                       s, n_rows, n_slots, n_heads, hkv, sc, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
+                       static_cast<const uint16_t*>(v), decay, state, state_out, slots, static_cast<uint16_t*>(o));
+    return hipGetLastError();
+  });
+  return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
+}
+
+}  // extern "C"

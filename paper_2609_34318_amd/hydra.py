@@ -60,6 +60,19 @@ class RopeC(ctypes.Structure):
                 ("inv_freq", ctypes.POINTER(ctypes.c_double))]
 
 
+class LinearC(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32),
+                ("d_k", ctypes.c_int32),
+                ("d_v", ctypes.c_int32),
+                ("scale", ctypes.c_float),
+                ("cu_seqlens", ctypes.POINTER(ctypes.c_int32)),
+                ("n_seqs", ctypes.c_int32),
+                ("q_tok_stride", ctypes.c_int32),
+                ("k_tok_stride", ctypes.c_int32),
+                ("v_tok_stride", ctypes.c_int32)]
+
+
 class SchedConfig(ctypes.Structure):
     _fields_ = [("n_ranks", ctypes.c_int32),
                 ("token_budget", ctypes.c_int64),
@@ -185,6 +198,15 @@ def lib() -> ctypes.CDLL:
         L.hydra_rope_q_bwd.argtypes = [R, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp]
         L.hydra_rope_kv_bwd.argtypes = [R, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
         for name in ("hydra_rope_q", "hydra_rope_kv", "hydra_rope_q_bwd", "hydra_rope_kv_bwd"):
+            getattr(L, name).restype = ctypes.c_int
+        N = ctypes.POINTER(LinearC)
+        L.hydra_linear_workspace_size.argtypes = [N]
+        L.hydra_linear_workspace_size.restype = sz
+        L.hydra_linear_plan.argtypes = [N, vp, sz, vp]
+        L.hydra_linear_fwd.argtypes = [N] + [vp] * 8 + [sz, i32, vp]
+        L.hydra_linear_bwd.argtypes = [N] + [vp] * 12 + [sz, i32, vp]
+        L.hydra_linear_step.argtypes = [i32] * 6 + [ctypes.c_float] + [vp] * 9
+        for name in ("hydra_linear_plan", "hydra_linear_fwd", "hydra_linear_bwd", "hydra_linear_step"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -697,6 +719,118 @@ def rope_kv_bwd(r: Rope, dk, dv, positions, d_kv, d_k_pe, cp_u: int = 1, stream=
     pp, pe_stride = _tok_rows(d_k_pe, "d_k_pe", r.cols)
     _check(lib().hydra_rope_kv_bwd(r.ref, T, H, d_nope, d_v, cp_u, gb, gp, vp, _positions(r, positions, T), dp,
                                    stride, pp, pe_stride, _stream(stream)), "hydra_rope_kv_bwd")
+
+
+# ------------------------------------------------------------------ linear attention
+
+class Linear:
+    """Linear attention with a decay for each head over packed sequences (hydra_linear.h): rows
+    cu_seqlens[s] .. cu_seqlens[s + 1] - 1 are sequence s."""
+
+    def __init__(self, cu_seqlens, n_heads: int, d_k: int = 128, d_v: int = 128, n_kv_heads: int = 0, scale: float = 0.0):
+        given = np.asarray(cu_seqlens)
+        self.cu = np.ascontiguousarray(given.astype(np.int32))
+        if self.cu.ndim != 1 or len(self.cu) < 2 or not np.array_equal(self.cu, given):
+            raise ValueError("cu_seqlens: a list of at least two integers of 32 bits is required")
+        self.n_seqs, self.n_tokens = len(self.cu) - 1, int(self.cu[-1])
+        self.n_heads, self.n_kv_heads, self.d_k, self.d_v = n_heads, n_kv_heads or n_heads, d_k, d_v
+        self.c = LinearC(n_heads=n_heads, n_kv_heads=n_kv_heads, d_k=d_k, d_v=d_v, scale=scale, n_seqs=self.n_seqs)
+        self.c.cu_seqlens = self.cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+    @property
+    def state_numel(self) -> int:
+        return self.n_seqs * self.n_heads * self.d_k * self.d_v
+
+
+def linear_workspace_size(p: Linear) -> int:
+    return int(lib().hydra_linear_workspace_size(p.ref))
+
+
+def linear_plan(p: Linear, workspace, stream=None):
+    """Uploads the work plan of p into workspace (outside any graph capture), for calls with planned=True."""
+    _here(workspace)
+    _check(lib().hydra_linear_plan(p.ref, _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                   _stream(stream)), "hydra_linear_plan")
+
+
+def _linear_rows(p: Linear, q, k, v) -> Tuple[int, int, int]:
+    """Checks q, k, v (tensors may have more rows than p) and records their token-row strides in it."""
+    out = []
+    for t, what, heads, d in ((q, "q", p.n_heads, p.d_k), (k, "k", p.n_kv_heads, p.d_k), (v, "v", p.n_kv_heads, p.d_v)):
+        ptr, stride = _rows(t, what, _more_rows(t, what, p.n_tokens), heads, d)
+        setattr(p.c, what + "_tok_stride", stride)
+        out.append(ptr)
+    return tuple(out)
+
+
+def _more_rows(t, what: str, rows: int) -> int:
+    if t.shape[0] < rows:
+        raise ValueError(f"{what}: {t.shape[0]} rows, at least {rows} needed")
+    return t.shape[0]
+
+
+def _dense_rows(t, what: str, rows: int, heads: int, d: int) -> Optional[int]:
+    """Address of a dense [rows or more, heads, d] bf16 tensor."""
+    if t is None:
+        return None
+    if tuple(t.shape[1:]) != (heads, d):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(rows, heads, d)}")
+    return _ptr(t, what, _BF16, _more_rows(t, what, rows) * heads * d)
+
+
+def linear_fwd(p: Linear, q, k, v, decay, o, workspace, state_in=None, state_out=None, planned=False, stream=None):
+    """o [T, H, d_v] bf16 (None: the last states alone) and, where given, state_out [n_seqs, H, d_k, d_v] float32 from
+    q [T, H, d_k], k [T, Hkv, d_k], v [T, Hkv, d_v] bf16 (token rows may be further apart than dense), the log decays
+    [H] float32 and the states that the sequences start from (None: zero; may be state_out).  Rows from
+    cu_seqlens[-1] on are left as they are.  workspace: a uint8 device tensor of linear_workspace_size(p), written by
+    the call; planned: it already holds p's plan, and only kernels are launched."""
+    _here(q, k, v, decay, o, workspace, state_in, state_out)
+    qp, kp, vp = _linear_rows(p, q, k, v)
+    _check(lib().hydra_linear_fwd(p.ref, qp, kp, vp, _ptr(decay, "decay", _F32, p.n_heads),
+                                  _ptr(state_in, "state_in", _F32, p.state_numel),
+                                  _dense_rows(o, "o", p.n_tokens, p.n_heads, p.d_v),
+                                  _ptr(state_out, "state_out", _F32, p.state_numel), _ptr(workspace, "workspace"),
+                                  workspace.numel() * workspace.element_size(), int(planned), _stream(stream)),
+           "hydra_linear_fwd")
+
+
+def linear_bwd(p: Linear, q, k, v, decay, d_o, dq, dk, dv, workspace, state_in=None, d_state_out=None, d_state_in=None,
+               planned=False, stream=None):
+    """Backward of linear_fwd: writes dq, dk, dv (bf16, as q, k, v, dense) and, where given, d_state_in, from d_o and the
+    gradients of the last states (None: zero)."""
+    _here(q, k, v, decay, d_o, dq, dk, dv, workspace, state_in, d_state_out, d_state_in)
+    qp, kp, vp = _linear_rows(p, q, k, v)
+    T, H, Hk = p.n_tokens, p.n_heads, p.n_kv_heads
+    _check(lib().hydra_linear_bwd(p.ref, qp, kp, vp, _ptr(decay, "decay", _F32, H),
+                                  _ptr(state_in, "state_in", _F32, p.state_numel), _dense_rows(d_o, "d_o", T, H, p.d_v),
+                                  _ptr(d_state_out, "d_state_out", _F32, p.state_numel),
+                                  _dense_rows(dq, "dq", T, H, p.d_k), _dense_rows(dk, "dk", T, Hk, p.d_k),
+                                  _dense_rows(dv, "dv", T, Hk, p.d_v),
+                                  _ptr(d_state_in, "d_state_in", _F32, p.state_numel), _ptr(workspace, "workspace"),
+                                  workspace.numel() * workspace.element_size(), int(planned), _stream(stream)),
+           "hydra_linear_bwd")
+
+
+def linear_step(q, k, v, decay, state, o, slots=None, state_out=None, scale: float = 0.0, stream=None):
+    """One token of every row's sequence: q [n, H, d_k], k [n, Hkv, d_k], v [n, Hkv, d_v] -> o [n, H, d_v], bf16.
+    state [n_slots, H, d_k, d_v] float32 is replaced (or state_out, of its shape, receives the new states).  slots:
+    int32 [n], the state of each row (None: row i has state i); rows whose slot is not in the pool are padding and are
+    left as they are; rows of one slot are taken in their order."""
+    _here(q, k, v, decay, state, o, slots, state_out)
+    n, H, d_k = q.shape
+    Hk, d_v = v.shape[1], v.shape[2]
+    out = state if state_out is None else state_out
+    if tuple(state.shape[1:]) != (H, d_k, d_v) or out.shape != state.shape:
+        raise ValueError(f"state: shape {tuple(state.shape)}, expected {('n_slots', H, d_k, d_v)}, and state_out the same")
+    _check(lib().hydra_linear_step(n, state.shape[0], H, Hk, d_k, d_v, scale, _ptr(q, "q", _BF16),
+                                   _ptr(k, "k", _BF16, n * Hk * d_k), _ptr(v, "v", _BF16, n * Hk * d_v),
+                                   _ptr(decay, "decay", _F32, H), _ptr(state, "state", _F32), _ptr(out, "state_out", _F32),
+                                   _ptr(slots, "slots", ("int32",), n), _ptr(o, "o", _BF16, n * H * d_v),
+                                   _stream(stream)), "hydra_linear_step")
 
 
 # ------------------------------------------------------------------ scheduler (host only)
