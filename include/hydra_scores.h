@@ -2,7 +2,7 @@
  * hydra_scores.h -- one rank's attention share with modified scores, on AMD MI355X (gfx950).
  *
  * The calls of hydra_attn.h for attention whose scores are capped, biased by distance, or seen
- * through a prefix mask.  For a visible pair of query i and key j of head h, at global positions
+ * through a prefix mask or a sliding window.  For a visible pair of query i and key j of head h, at global positions
  * p_i and p_j:
  *
  *   s_ij = softmax_scale <q_i, k_j>
@@ -14,7 +14,12 @@
  *   p_j <= p_i  or  p_j < cu_seqlens[d] + prefix_len[d]
  *
  * (a document's first prefix_len[d] tokens are seen by all of its tokens, themselves included; the
- * others as in hydra_attn.h).  LSE, O, the merge of ring steps and D are those of hydra_attn.h for these
+ * others as in hydra_attn.h); or, with a window of w keys and n sinks, iff both lie in one document d and
+ *
+ *   p_j <= p_i  and  (p_i - p_j < w  or  p_j < cu_seqlens[d] + n)
+ *
+ * (the last w keys up to its own, and the document's first n keys).  What no query of a tile sees is not visited: the
+ * work grows with the window.  A ring step whose keys lie behind every window leaves O = 0 and LSE = -inf.  LSE, O, the merge of ring steps and D are those of hydra_attn.h for these
  * scores.  Backward, with P = exp(s - LSE) and t = tanh(softmax_scale <q_i, k_j> / c):
  *
  *   dV = P^T dO,  dS = P o (dO V^T - D) o (1 - t^2),  dQ = softmax_scale dS K,  dK = softmax_scale dS^T Q
@@ -52,6 +57,9 @@ typedef struct {
                                  the kernels run                                               */
   const int32_t* prefix_len;  /* NULL for none, or HOST int32[n_docs], 0 .. the document's
                                  length; read only during the call, part of the plan           */
+  int32_t window;             /* w: 0 for none, and then sinks must be 0; else prefix_len must be NULL.
+                                 Both part of the plan                                         */
+  int32_t sinks;              /* n >= 0                                                        */
 } hydra_scores_t;
 
 /* hydra_workspace_size, hydra_split_scratch_size, hydra_bwd_ds_bytes, hydra_visible_pairs and
@@ -63,8 +71,8 @@ int64_t hydra_scores_visible_pairs(const hydra_problem_t* p, const hydra_scores_
 int64_t hydra_scores_plan_items(const hydra_problem_t* p, const hydra_scores_t* sc, int32_t which, int32_t* out,
                                 int64_t cap);
 
-/* hydra_attn_plan: the plan, and the workspace's size, depend on the prefixes (NULL is 0 for every document) and on
- * whether the scores are modified at all, not on the cap or the slopes: planned calls may turn either on, off or to
+/* hydra_attn_plan: the plan, and the workspace's size, depend on the prefixes (NULL is 0 for every document), the
+ * window and its sinks, and on whether the scores are modified at all, not on the cap or the slopes: planned calls may turn either on, off or to
  * another value on one plan, but not the last modification off or the first one on (HYDRA_ERR_WORKSPACE). */
 int hydra_scores_plan(const hydra_problem_t* p, const hydra_scores_t* sc, void* workspace, size_t workspace_bytes,
                       void* stream);

@@ -7,7 +7,8 @@ Scores: for query i and key j of one document at global positions p_i and p_j,
 
     s_ij = tau <q_i, k_j>,  s_ij = c tanh(s_ij / c) with a cap,  s_ij = s_ij - slope_h |p_i - p_j| with slopes,
 
-visible where p_j <= p_i or p_j lies in the document's prefix.  LSE, O and D as in attention.py; backward
+visible where p_j <= p_i or p_j lies in the document's prefix, or with a window of w keys and n sinks where p_j <= p_i
+and (p_i - p_j < w or p_j is one of the document's first n).  LSE, O and D as in attention.py; backward
 
     dS_ij = P_ij (<dO_i, v_j> - D_i) (1 - tanh^2),  dQ = tau dS K,  dK = tau dS^T Q,  dV = P^T dO.
 
@@ -22,13 +23,16 @@ import numpy as np
 from .attention import doc_of, row_positions
 
 
-def visible(cu_seqlens, q_segs, kv_segs, prefix=None) -> np.ndarray:
+def visible(cu_seqlens, q_segs, kv_segs, prefix=None, window=0, sinks=0) -> np.ndarray:
     """[Nq, Nk] truth values."""
     cu = np.asarray(cu_seqlens, dtype=np.int64)
     qp, kp = row_positions(q_segs), row_positions(kv_segs)
     if len(qp) == 0 or len(kp) == 0:
         return np.zeros((len(qp), len(kp)), bool)
     qd, kd = doc_of(cu, qp), doc_of(cu, kp)
+    if window:
+        near = (qp[:, None] - kp[None] < window) | (kp[None] < (cu[:-1] + sinks)[qd][:, None])
+        return (qd[:, None] == kd[None]) & (kp[None] <= qp[:, None]) & near
     end = cu[:-1] + (0 if prefix is None else np.asarray(prefix, dtype=np.int64))
     return (qd[:, None] == kd[None]) & ((kp[None] <= qp[:, None]) | (kp[None] < end[qd][:, None]))
 
@@ -44,12 +48,14 @@ def _scores(q, k, scale, softcap, slope, qp, kp, vis):
     return np.where(vis, s, -np.inf), 1.0 - t * t
 
 
-def attn_fwd(q, k, v, cu_seqlens, q_segs, kv_segs, scale=None, softcap=0.0, slopes=None, prefix=None):
+def attn_fwd(q, k, v, cu_seqlens, q_segs, kv_segs, scale=None, softcap=0.0, slopes=None, prefix=None, window=0,
+             sinks=0):
     """O [Nq, H, dv] and LSE [H, Nq] of q [Nq, H, dqk], k [Nk, Hkv, dqk], v [Nk, Hkv, dv]."""
     q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
     H, grp = q.shape[1], q.shape[1] // k.shape[1]
     tau = 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale)
-    vis, qp, kp = visible(cu_seqlens, q_segs, kv_segs, prefix), row_positions(q_segs), row_positions(kv_segs)
+    vis = visible(cu_seqlens, q_segs, kv_segs, prefix, window, sinks)
+    qp, kp = row_positions(q_segs), row_positions(kv_segs)
     O, L = np.zeros((q.shape[0], H, v.shape[2])), np.full((H, q.shape[0]), -np.inf)
     seen = vis.any(axis=1)
     if not seen.any():
@@ -65,12 +71,14 @@ def attn_fwd(q, k, v, cu_seqlens, q_segs, kv_segs, scale=None, softcap=0.0, slop
     return O, L
 
 
-def attn_bwd(q, k, v, o, lse, do, cu_seqlens, q_segs, kv_segs, scale=None, softcap=0.0, slopes=None, prefix=None):
+def attn_bwd(q, k, v, o, lse, do, cu_seqlens, q_segs, kv_segs, scale=None, softcap=0.0, slopes=None, prefix=None, window=0,
+             sinks=0):
     """dQ, dK, dV of one ring step from the final O and LSE of the rows."""
     q, k, v, o, lse, do = (np.asarray(x, dtype=np.float64) for x in (q, k, v, o, lse, do))
     H, grp = q.shape[1], q.shape[1] // k.shape[1]
     tau = 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale)
-    vis, qp, kp = visible(cu_seqlens, q_segs, kv_segs, prefix), row_positions(q_segs), row_positions(kv_segs)
+    vis = visible(cu_seqlens, q_segs, kv_segs, prefix, window, sinks)
+    qp, kp = row_positions(q_segs), row_positions(kv_segs)
     dQ, dK, dV = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
     for h in range(H):
         g = h // grp

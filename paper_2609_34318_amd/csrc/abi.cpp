@@ -172,7 +172,7 @@ Launch list_launch(void* ws, size_t whole, int64_t n_whole, const ListSize& l, c
 }
 
 std::vector<int64_t> plan_key(const Problem& pr) {
-  std::vector<int64_t> k = {pr.H, pr.Hkv, int64_t(pr.cu.size()), int64_t(pr.pe.size())};
+  std::vector<int64_t> k = {pr.H, pr.Hkv, int64_t(pr.cu.size()), int64_t(pr.pe.size()), pr.window, pr.sinks};
   k.insert(k.end(), pr.cu.begin(), pr.cu.end());
   k.insert(k.end(), pr.pe.begin(), pr.pe.end());
   for (const hydra_chunk_t* c : {&pr.q, &pr.kv}) {
@@ -253,6 +253,8 @@ ScoreArgs score_args(const Problem& pr, const AttnArgs& base, bool backward) {
   static_cast<AttnArgs&>(a) = base;
   a.pe = base.cu + pr.cu.size();
   a.slopes = pr.slopes;
+  a.window = pr.window;
+  a.sinks = pr.sinks;
   if (pr.softcap > 0.f) {
     constexpr double log2e = 1.4426950408889634074;
     const double in = double(pr.scale) / double(pr.softcap), cap = double(pr.softcap) * log2e, out = backward ? 1 : cap;

@@ -89,6 +89,7 @@ __device__ __forceinline__ void dq_issue(lds_char* stage, const AttnArgs& a, con
 // stage 0 | stage 1; before the loop the waves' Q, then dO rows from the start of stage 1, after it
 // their outputs
 constexpr int DQ_LDS = DQ_STAGE + DQ_WAVES * own_bytes<DQK>();
+constexpr int DQ_STARTS = DQ_WAVES * 64 * 4;  // behind them with a window: each lane's document start, read where sinks are
 static_assert(DQ_LDS >= DQ_NSTAGE * DQ_STAGE && DQ_LDS >= DQ_WAVES * ROWS_OUT_BYTES, "LDS");
 
 template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& a, int block, lds_char* smem) {
@@ -118,10 +119,11 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   const int mc = q_n > 0 ? min(m, q_n - 1) : -32 * wave;
   float lse2 = a.lse2[(int64_t)head * a.nq + q_row0 + mc];
   float neg_D = a.Dvec[(int64_t)head * a.nq + q_row0 + mc];
-  int lo_q, hi_row = 0, hi_first, hi_last;  // as in the forward; hi_row: of this lane's row
+  int lo_q, hi_row = 0, hi_first, hi_last, start_q = 0;  // as in the forward; hi_row: of this lane's row
   if constexpr (MOD != kPlain) {
-    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, q_pos0 + mc);
+    const Span see = row_span<false, MOD>(a, it.d0, it.d1, q_pos0 + mc);
     lo_q = see.lo;
+    start_q = see.start;
     hi_row = see.hi;
     hi_first = __builtin_amdgcn_readfirstlane(see.hi);
     hi_last = q_n > 0 ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
@@ -132,6 +134,9 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
   }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
+  const Sinks sinks = wave_sinks<MOD>(a, start_q, q_n > 0);
+  if constexpr (MOD & kWindow)
+    *reinterpret_cast<__attribute__((address_space(3))) int*>(smem + DQ_LDS + (wave * 64 + lane) * 4) = start_q;
   const float slope = slope_log2<MOD>(a, head);
   settle(lse2);
   settle(neg_D);
@@ -177,7 +182,8 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
       dq_issue(smem + ((t + 1) % DQ_NSTAGE) * DQ_STAGE, a, cur, kv_head, wave);
     }
     // a wave none of whose rows sees the tile leaves the matrix cores to the others
-    if (kpos >= hi_last || kpos + kn <= lo_first) continue;
+    const bool at_sinks = (MOD & kWindow) && sinks.touch(kpos, kn);
+    if ((kpos >= hi_last || kpos + kn <= lo_first) && !at_sinks) continue;
     const bool full = (kn == DQ_BK) && (lo_last <= kpos) && (kpos + DQ_BK <= hi_first);
 
     static_for<DQ_BK / 32>([&](auto kb_) {
@@ -234,10 +240,17 @@ template <int MOD> __device__ __forceinline__ void bwd_dq_body(const Args<MOD>& 
         const int hi_q = (ml & 31) < q_n ? (MOD != kPlain ? hi_row : q_pos0 + (ml & 31) + 1) : 0;
         const int base = kpos - lo_q + 32 * kb + 8 * (ml >> 5);
         const int lim = max(0, min(hi_q, kpos + kn) - lo_q);
+        int base_s = 0, lim_s = 0;  // the same of the row's sinks
+        if (at_sinks) {
+          const int start = *reinterpret_cast<const __attribute__((address_space(3))) int*>(smem + DQ_LDS + (wave * 64 + ml) * 4);
+          base_s = kpos - start + 32 * kb + 8 * (ml >> 5);
+          lim_s = max(0, min(sinks.n, min(hi_q, kpos + kn) - start));
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int r = base + 16 * (e >> 3) + (e & 7);
-          const bool vis = (unsigned)r < (unsigned)lim;
+          bool vis = (unsigned)r < (unsigned)lim;
+          if constexpr (MOD & kWindow) vis |= (unsigned)(base_s + r - base) < (unsigned)lim_s;
           const float p = __builtin_amdgcn_exp2f(vis ? arg(e) : -INFINITY);
           ds[e] = (MOD & kCap) ? mul_zero(p, dpd(e)) : p * dpd(e);
         }
@@ -361,7 +374,7 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
   // pair's first one and those from lo_last on its last
   int lo_k, hi_k, lo_first, lo_last;
   if constexpr (MOD != kPlain) {
-    const Span seen = row_span<true>(a.cu, a.pe, it.d0, it.d1, k_pos0 + min(kj, k_n - 1));
+    const Span seen = row_span<true, MOD>(a, it.d0, it.d1, k_pos0 + min(kj, k_n - 1));
     lo_k = k_valid ? seen.lo : 0x7fffffff;
     hi_k = seen.hi;
     lo_first = __builtin_amdgcn_readfirstlane(seen.lo);
@@ -372,9 +385,10 @@ __device__ __forceinline__ void bwd_dkdv_body(const Args<MOD>& a, int block, lds
     lo_first = k_pos0 + pair * 32;
     lo_last = lo_first + kn_w - 1;
   }
-  // document ends of the pair's first and last key (lanes past the end repeat the last one)
-  const int hi_first = __builtin_amdgcn_readfirstlane(hi_k);
-  const int hi_last = __builtin_amdgcn_readlane(hi_k, 31);
+  // document ends of the pair's first and last key (lanes past the end repeat the last one); with a window the least
+  // and the greatest end of its keys' rows
+  const int hi_first = (MOD & kWindow) ? span_min(hi_k) : __builtin_amdgcn_readfirstlane(hi_k);
+  const int hi_last = (MOD & kWindow) ? span_max(hi_k) : __builtin_amdgcn_readlane(hi_k, 31);
   const float sl2 = log2_unit<MOD>(a);
   const int qoff = dma_lane_off<DQK>(a.q_s, head0, pair, lane);  // role B's copy lanes (wave b = pair)
   const int ooff = dma_lane_off<DV>(a.H * DV, head0, pair, lane);
@@ -649,7 +663,8 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dkdv_ds_kernel(
 // the end together, lost where workgroups are long (64K: 79.3 to 83.2 ms): dK/dV's and dQ's tiles then
 // share the L2s.  Up to seven places after dK/dV stay empty, so that dQ's heads keep their XCDs.
 template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_recompute_kernel(Args<MOD> q, Args<MOD> kv) {
-  __shared__ __attribute__((aligned(1024))) char smem_raw[DQ_LDS > KV_LDS ? DQ_LDS : KV_LDS];
+  constexpr int DQ_BYTES = DQ_LDS + ((MOD & kWindow) ? DQ_STARTS : 0);
+  __shared__ __attribute__((aligned(1024))) char smem_raw[DQ_BYTES > KV_LDS ? DQ_BYTES : KV_LDS];
   lds_char* smem = (lds_char*)smem_raw;
   const int nkv = kv.n_items * kv.kv_heads;
   const int b = blockIdx.x, q0 = (nkv + N_XCD - 1) / N_XCD * N_XCD;
@@ -689,6 +704,7 @@ struct DsTile {
 struct DsWalk {
   int rr, r, end, kpos_r, j;  // range, next key row, the range's end, key position - key row, record
   int lo_first, hi_last;      // first position that the wave's first row sees, one past its last row's last (0: no rows)
+  Sinks sinks;                // with a window, what else they see
   i32x16 rec;
 };
 
@@ -728,7 +744,7 @@ __device__ __forceinline__ DsTile ds_next(const AttnArgs& a, const DsRanges R, D
   // the sub-block of the item's query tiling that holds the wave's rows [qrow, qrow + 32)
   d.off = -1;
   const int kpos = d.krow0 + w.kpos_r;  // a key item lies in one segment: its rows' positions are consecutive
-  if (kpos < w.hi_last && kpos + d.kn > w.lo_first) {
+  if ((kpos < w.hi_last && kpos + d.kn > w.lo_first) || w.sinks.touch(kpos, d.kn)) {
     int slot = w.rec[3];
 #pragma unroll
     for (int k = 0; k < MAX_RANGES; ++k) {
@@ -746,7 +762,7 @@ __device__ __forceinline__ DsTile ds_next(const AttnArgs& a, const DsRanges R, D
   return d;
 }
 
-// MOD: kPlain or kScored; what else the scores have lies in the stored dS.
+// MOD: kPlain, kScored or kScored with kWindow; what else the scores have lies in the stored dS.
 template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Args<MOD> a) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[DQS_LDS];
   lds_char* smem = (lds_char*)smem_raw;
@@ -769,10 +785,12 @@ template <int MOD> __global__ __launch_bounds__(512, 1) void bwd_dq_ds_kernel(Ar
   walk.r = 0;
   walk.end = 0;
   if constexpr (MOD != kPlain) {
-    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, it.pos0 + (wave_rows ? 32 * wave + m : 0));
+    const Span see = row_span<false, MOD>(a, it.d0, it.d1, it.pos0 + (wave_rows ? 32 * wave + m : 0));
+    walk.sinks = wave_sinks<MOD>(a, see.start, wave_rows);
     walk.lo_first = __builtin_amdgcn_readfirstlane(see.lo);
     walk.hi_last = wave_rows ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
   } else {
+    walk.sinks = {0, 0, 0};
     walk.hi_last = wave_rows ? it.pos0 + 32 * wave + 32 : 0;
     walk.lo_first = __builtin_amdgcn_readfirstlane(
         doc_edge<false>(a.cu, it.d0, it.d1, it.edge0, it.pos0 + (wave_rows ? 32 * wave : 0)));
@@ -984,7 +1002,7 @@ hipError_t launch_bwd(const Args<MOD>& a, int o_bytes, const Launch& q_whole, co
           hipSuccess)
         return e;
       if ((e = launch_merges<MOD>(b, 0, b, kv.n_merges, stream)) != hipSuccess) return e;
-      if ((e = launch_list(bwd_dq_ds_kernel<plain ? kPlain : kScored>, plain ? "bwd_dq_ds" : "bwd_dq_ds_scores",
+      if ((e = launch_list(bwd_dq_ds_kernel<plain ? kPlain : MOD & (kScored | kWindow)>, plain ? "bwd_dq_ds" : "bwd_dq_ds_scores",
                            list_args(b, q_whole, nullptr), G * a.grp, stream)) != hipSuccess)
         return e;
     }

@@ -138,11 +138,12 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
 
   // the first position that this lane's row, the wave's first and its last row see (rows past the end
   // repeat the last one), and the one past their last
-  int lo_q, hi_q, hi_first, hi_last;
+  int lo_q, hi_q, hi_first, hi_last, start_q = 0;
   const int row_pos = q_pos0 + min(m, max(q_n, 1) - 1);
   if constexpr (MOD != kPlain) {
-    const Span see = row_span<false>(a.cu, a.pe, it.d0, it.d1, row_pos);
+    const Span see = row_span<false, MOD>(a, it.d0, it.d1, row_pos);
     lo_q = see.lo;
+    start_q = see.start;
     hi_first = __builtin_amdgcn_readfirstlane(see.hi);
     hi_last = q_n > 0 ? __builtin_amdgcn_readlane(see.hi, 31) : 0;
     hi_q = q_valid ? see.hi : 0;
@@ -154,6 +155,7 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
   }
   const int lo_first = __builtin_amdgcn_readfirstlane(lo_q);
   const int lo_last = __builtin_amdgcn_readlane(lo_q, 31);
+  const Sinks sinks = wave_sinks<MOD>(a, start_q, q_n > 0);
   const float slope2 = slope_log2<MOD>(a, head);
   bf16x8 qf[DQK / 16];
   wait_dma();
@@ -180,7 +182,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
     }
     // a wave none of whose rows sees the tile (the diagonal's upper half, another document)
     // leaves the matrix cores to the others
-    if (kpos >= hi_last || kpos + kn <= lo_first) continue;
+    const bool at_sinks = (MOD & kWindow) && sinks.touch(kpos, kn);
+    if ((kpos >= hi_last || kpos + kn <= lo_first) && !at_sinks) continue;
 
     f32x16 s[2];
 #pragma unroll
@@ -223,13 +226,24 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 1) void attn_fwd_kernel(Args<MOD> a
       // 0 <= base + c(e) < lim with base = kpos - lo_q + 8*hh
       const int base = kpos - lo_q + 8 * hh;
       const int lim = max(0, min(hi_q, kpos + kn) - lo_q);
+      if (at_sinks) {  // or iff it is one of the row's sinks
+        const int base_s = kpos - start_q + 8 * hh, lim_s = max(0, min(sinks.n, min(hi_q, kpos + kn) - start_q));
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int r = base + 32 * kb + 16 * (e >> 3) + (e & 7);
-          s[kb][e] = (unsigned)r < (unsigned)lim ? s[kb][e] : -INFINITY;
-        }
+          for (int e = 0; e < 16; ++e) {
+            const int c = 32 * kb + 16 * (e >> 3) + (e & 7);
+            s[kb][e] = (unsigned)(base + c) < (unsigned)lim || (unsigned)(base_s + c) < (unsigned)lim_s ? s[kb][e] : -INFINITY;
+          }
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int r = base + 32 * kb + 16 * (e >> 3) + (e & 7);
+            s[kb][e] = (unsigned)r < (unsigned)lim ? s[kb][e] : -INFINITY;
+          }
+      }
     }
     // row max as four independent chains that take two new values per step (one
     // three-input maximum each)

@@ -720,6 +720,7 @@ struct AttnArgs {
 // ... with modified scores (hydra_scores.h)
 struct ScoreArgs : AttnArgs {
   const int* pe;        // prefix end of each document
+  int window, sinks;    // with kWindow: a row sees the last `window` keys up to its own and its document's first `sinks`
   const float* slopes;  // [H], or null
   // a cap c (out = 0: none), of raw scores s: out tanh(s scale / c) = s (poly[0] + poly[1] s^2 + ...) up to
   // |s| = near, and s (low[0] + ...) up to |s| = small
@@ -738,8 +739,8 @@ constexpr double TANH_LOW[3] = {0.9999996, -0.33321908, 0.12841613};
 constexpr float P_LOG2 = 15.f;
 
 // What a kernel does to its scores: nothing (the plain kernels), or kScored (the prefix mask) with any of
-// the others.
-enum Mod { kPlain = 0, kScored = 1, kCap = 2, kBias = 4 };
+// the others; kWindow is a mask in the prefix's place.
+enum Mod { kPlain = 0, kScored = 1, kCap = 2, kBias = 4, kWindow = 8 };
 template <int MOD> struct ArgsFor { typedef ScoreArgs type; };
 template <> struct ArgsFor<kPlain> { typedef AttnArgs type; };
 template <int MOD> using Args = typename ArgsFor<MOD>::type;

@@ -10,7 +10,9 @@
 // masked (Sec. 2.2) and is never visited.  With prefixes a row at p of document d sees
 // [doc_start(d), max(p + 1, prefix end(d))), whose ends grow with p too: the intervals end at the
 // last row's prefix where that is later, and a key tile that starts in a prefix is seen from its
-// document's start.  Tiles are ordered heaviest first, the kernel-level counterpart of the scheduler
+// document's start.  With a window of w keys a row sees [max(doc_start, p - w + 1), p] and its document's first keys
+// (sinks): of a query tile the sinks of its first row's document are an interval of their own (later documents start
+// inside the tile), and a key tile without sinks of its last document is seen up to w - 1 behind its last key.  Tiles are ordered heaviest first, the kernel-level counterpart of the scheduler
 // placing the longest sequences first (Sec. 5.1.1, Alg. 1, phase 2).
 #include "plan.h"
 
@@ -26,6 +28,8 @@ namespace hydra {
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
+// Sinks that end less than this before a query tile's window are walked with it.
+constexpr int64_t kNearSinks = 128;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -156,7 +160,10 @@ int check_problem(const hydra_problem_t* p, Problem* out) {
 
 int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* out) {
   const int rc = check_problem(p, out);
-  if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len)) return rc;
+  if (rc != HYDRA_OK || !sc || (sc->softcap == 0.f && !sc->slopes && !sc->prefix_len && sc->window == 0 && sc->sinks == 0))
+    return rc;
+  // a prefix is seen through no window, and without a window every first key stays visible
+  if (sc->window < 0 || sc->sinks < 0 || (sc->window == 0 ? sc->sinks > 0 : sc->prefix_len != nullptr)) return HYDRA_ERR_INVALID;
   // the constants of a capped kernel are softmax_scale times powers of softmax_scale / cap up to the eighth (forward),
   // and those powers up to the ninth (backward): within these all are normal numbers but the last, which has 17
   // bits at the least and adds no more than 2^-9 of the sum
@@ -171,6 +178,8 @@ int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* o
     out->pe[d] += sc->prefix_len[d];
   }
   out->scored = true;
+  out->window = sc->window;
+  out->sinks = sc->sinks;
   out->softcap = sc->softcap;
   out->slopes = sc->slopes;
   return HYDRA_OK;
@@ -191,19 +200,42 @@ void plan_items(const Problem& pr, int which, std::vector<int32_t>* items) {
     it[1] = t.pos0;
     it[2] = t.n;
     const int64_t first = t.pos0, last = int64_t(t.pos0) + t.n - 1;
-    int64_t lo, hi;
+    int64_t lo, hi, sink0 = 0, sink1 = -1;
     if (which == 0) {  // keys seen by queries [first, last]
       lo = pr.cu[doc_index(pr.cu, first)];
       hi = last;
       if (pr.scored) hi = std::max<int64_t>(hi, int64_t(pr.pe[size_t(doc_index(pr.cu, last))]) - 1);
+      if (pr.window > 0 && first - pr.window + 1 > lo) {
+        // the sinks apart, unless they are near: the stored dS is read 64 keys at a time, which no two ranges may share
+        const int64_t start = lo, from = first - pr.window + 1;
+        if (pr.sinks == 0 || from >= start + pr.sinks + kNearSinks) {
+          lo = from;
+          sink0 = start;
+          sink1 = start + pr.sinks - 1;
+        }
+      }
     } else {           // queries that see keys [first, last]
       lo = first;
       hi = int64_t(pr.cu[doc_index(pr.cu, last) + 1]) - 1;
       // a prefix key is seen from its document's start on; in whole blocks of 32 rows, as the stored dS is
       // laid out (the rows before the document are masked)
       if (const size_t d = size_t(doc_index(pr.cu, first)); pr.scored && first < pr.pe[d]) lo = pr.cu[d] & ~31;
+      if (const int64_t start = pr.cu[size_t(doc_index(pr.cu, last))];
+          pr.window > 0 && std::max(first, start) - start >= pr.sinks)
+        hi = std::min<int64_t>(hi, last + pr.window - 1);
     }
-    it[3] = ranges_in(other, lo, hi, it + 4);
+    if (sink0 <= sink1) {
+      int32_t two[6 * HYDRA_MAX_SEGS];
+      const int n0 = ranges_in(other, sink0, sink1, two), n1 = ranges_in(other, lo, hi, two + 3 * n0);
+      if (n0 + n1 <= HYDRA_MAX_SEGS) {
+        it[3] = n0 + n1;
+        std::copy(two, two + 3 * (n0 + n1), it + 4);
+      } else {  // too many for a record: from the document's start on
+        it[3] = ranges_in(other, sink0, hi, it + 4);
+      }
+    } else {
+      it[3] = ranges_in(other, lo, hi, it + 4);
+    }
     for (int r = 0; r < it[3]; ++r) cost[i] += it[4 + 3 * r + 2];
   }
   std::vector<size_t> order(n);
@@ -383,6 +415,12 @@ int64_t visible_pairs(const Problem& pr) {
       for (int d = std::max(d0, 0); d <= d1 && d < n_docs; ++d) {
         const int64_t da = pr.cu[d], db = pr.cu[d + 1];
         const int64_t q0 = std::max(qa, da), q1 = std::min(qb, db), k0 = std::max(ka, da), k1 = std::min(kb, db);
+        if (pr.window > 0) {  // the causal pairs but those behind the window, and of these the sinks
+          const int64_t w = pr.window;
+          total += causal_pairs(q0, q1, k0, k1) - causal_pairs(q0 - w, q1 - w, k0, k1) +
+                   causal_pairs(q0 - w, q1 - w, k0, std::min(k1, da + pr.sinks));
+          continue;
+        }
         const int64_t pe = pr.scored ? pr.pe[size_t(d)] : da;
         if (q1 > q0) total += (q1 - q0) * std::max<int64_t>(0, std::min(k1, pe) - k0);
         total += causal_pairs(q0, q1, std::max(k0, pe), k1);

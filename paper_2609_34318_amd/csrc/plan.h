@@ -30,6 +30,7 @@ struct Problem {
   float softcap = 0.f;
   const float* slopes = nullptr;
   std::vector<int32_t> pe;     // n_docs prefix ends: keys before it are seen by the whole document
+  int window = 0, sinks = 0;   // a sliding window (0: none; then no prefixes) and the first keys that stay visible
 };
 
 // Returns HYDRA_OK or an error status; fills `out` on success.

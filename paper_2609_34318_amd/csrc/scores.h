@@ -11,12 +11,14 @@ namespace hydra {
 
 // Positions [lo, hi) of the keys that the query at `pos` sees, or (KEYS) of the queries that see the key at
 // `pos`, which lies in one of documents d0 .. d1.  Both ends grow with pos, so a tile's first and last row
-// bound what any of its rows sees.
+// bound what any of its rows sees.  With a window a query also sees the keys before its lo at less than `sinks` from
+// its document's start, and of keys hi does not grow: a sink is seen to its document's end (span_min, span_max).
 struct Span {
-  int lo, hi;
+  int lo, hi, start;  // start: of the document
 };
-template <bool KEYS>
-__device__ __forceinline__ Span row_span(const int* __restrict__ cu, const int* __restrict__ pe, int d0, int d1, int pos) {
+template <bool KEYS, int MOD>
+__device__ __forceinline__ Span row_span(const Args<MOD>& a, int d0, int d1, int pos) {
+  const int *__restrict__ cu = a.cu, *__restrict__ pe = a.pe;
   int start, end, prefix;
   if (d1 - d0 <= 8) {
     start = ((cint*)cu)[d0];
@@ -40,8 +42,35 @@ __device__ __forceinline__ Span row_span(const int* __restrict__ cu, const int* 
     prefix = pe[lo];
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(start), "+v"(end), "+v"(prefix)::"memory");
   }
-  if (KEYS) return {pos < prefix ? start : pos, end};
-  return {start, max(pos + 1, prefix)};
+  if constexpr (MOD & kWindow) {
+    if (KEYS) return {pos, pos - start >= a.sinks && end - pos > a.window ? pos + a.window : end, start};
+    return {max(start, pos - a.window + 1), pos + 1, start};
+  }
+  if (KEYS) return {pos < prefix ? start : pos, end, start};
+  return {start, max(pos + 1, prefix), start};
+}
+
+// The smallest and the largest of a wave's values.
+__device__ __forceinline__ int span_min(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = min(x, __shfl_xor(x, d, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int span_max(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = max(x, __shfl_xor(x, d, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// The sinks of a wave's rows, whose documents start at `first` to `last` (n = 0: none, or no rows).
+struct Sinks {
+  int n, first, last;
+  __device__ __forceinline__ bool touch(int kpos, int kn) const { return n > 0 && kpos - last < n && kpos + kn > first; }
+};
+template <int MOD> __device__ __forceinline__ Sinks wave_sinks(const Args<MOD>& a, int start, bool rows) {
+  if constexpr (MOD & kWindow)
+    return {rows ? a.sinks : 0, __builtin_amdgcn_readfirstlane(start), __builtin_amdgcn_readlane(start, 31)};
+  return {0, 0, 0};
 }
 
 // The slope of a head in log2 units, finite: an infinite one times the distance 0 of a row's own key is NaN.
@@ -193,9 +222,12 @@ __device__ __forceinline__ bf16x8 to_f16x8(const float* v) {
 }
 
 // f with the variant of a problem's scores as a compile-time number.
+template <int MASK, class F> hipError_t with_mask(const ScoreArgs& a, F&& f) {
+  if (a.out > 0.f) return a.slopes ? f(IntC<MASK | kCap | kBias>{}) : f(IntC<MASK | kCap>{});
+  return a.slopes ? f(IntC<MASK | kBias>{}) : f(IntC<MASK>{});
+}
 template <class F> hipError_t with_mod(const ScoreArgs& a, F&& f) {
-  if (a.out > 0.f) return a.slopes ? f(IntC<kScored | kCap | kBias>{}) : f(IntC<kScored | kCap>{});
-  return a.slopes ? f(IntC<kScored | kBias>{}) : f(IntC<kScored>{});
+  return a.window > 0 ? with_mask<kScored | kWindow>(a, f) : with_mask<kScored>(a, f);
 }
 
 }  // namespace hydra

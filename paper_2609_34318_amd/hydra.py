@@ -45,7 +45,9 @@ class ProblemC(ctypes.Structure):
 class ScoresC(ctypes.Structure):
     _fields_ = [("softcap", ctypes.c_float),
                 ("slopes", ctypes.c_void_p),
-                ("prefix_len", ctypes.POINTER(ctypes.c_int32))]
+                ("prefix_len", ctypes.POINTER(ctypes.c_int32)),
+                ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32)]
 
 
 ROPE_MAX_AXES = 4
@@ -227,11 +229,16 @@ def _chunk(segs: Sequence[Tuple[int, int]]) -> Chunk:
 class Scores:
     """How a problem's scores are modified: capped by a tanh (softcap), biased by minus slope times the
     distance of query and key (slopes: float32 device tensor, one per query head), and a prefix of each
-    document that all of its tokens see (prefix: a length per document).  The cap and the slopes are
+    document that all of its tokens see (prefix: a length per document) or a sliding window (a token sees the
+    last `window` keys up to its own and its document's first `sinks`).  The cap and the slopes are
     constants: they get no gradient."""
 
-    def __init__(self, softcap: float = 0.0, slopes=None, prefix: Optional[Sequence[int]] = None):
+    def __init__(self, softcap: float = 0.0, slopes=None, prefix: Optional[Sequence[int]] = None, window: int = 0,
+                 sinks: int = 0):
         self.softcap, self.slopes = float(softcap), slopes
+        self.window, self.sinks = int(window), int(sinks)
+        if not (0 <= self.window < 1 << 31 and 0 <= self.sinks < 1 << 31) or self.window != window or self.sinks != sinks:
+            raise ValueError(f"window {window}, sinks {sinks}: integers of 32 bits, not negative, are required")
         self.prefix = None
         if prefix is not None:
             given = np.asarray(prefix)
@@ -239,7 +246,7 @@ class Scores:
             if not np.array_equal(self.prefix, given):
                 raise ValueError("prefix: lengths must be integers of 32 bits")
         self.c = ScoresC()
-        self.c.softcap = self.softcap
+        self.c.softcap, self.c.window, self.c.sinks = self.softcap, self.window, self.sinks
         if self.softcap and not self.c.softcap:  # no cap to the library
             raise ValueError(f"softcap: {self.softcap} is 0 in 32 bits")
         if slopes is not None:
@@ -249,7 +256,7 @@ class Scores:
 
     @property
     def any(self) -> bool:
-        return self.softcap != 0 or self.slopes is not None or self.prefix is not None
+        return self.softcap != 0 or self.slopes is not None or self.prefix is not None or self.window != 0
 
 
 class Problem:
