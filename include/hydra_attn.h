@@ -268,7 +268,9 @@ void hydra_tile_rows(int32_t* q_tile_rows, int32_t* kv_tile_rows);
  * "bwd_recompute" (dK/dV and dQ), "bwd_dkdv_ds" and "bwd_dq_ds" (stored dS), "bwd_merge" (parts of
  * split items), with modified scores (hydra_scores.h) "attn_fwd_scores", "bwd_recompute_scores",
  * "bwd_dkdv_ds_scores" and "bwd_dq_ds_scores" in place of those, for the calls of hydra_rope.h "rope_q",
- * "rope_kv", "rope_q_bwd" and "rope_kv_bwd", and for those of hydra_layout.h and hydra_gate.h "pack_heads",
+ * "rope_kv", "rope_q_bwd" and "rope_kv_bwd", of hydra_linear.h "linear_states", "linear_scan", "linear_fwd",
+ * "linear_bwd", "linear_groups" and "linear_step", of hydra_norm.h "unpack_normed", "pack_normed_bwd" and
+ * "norm_weights", and for those of hydra_layout.h and hydra_gate.h "pack_heads",
  * "unpack_heads", "zigzag_gather", "zigzag_scatter", "unpack_gated", "pack_gated_bwd". */
 typedef struct {
   char    name[32];

@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhydra_attn.so")
 SOURCES = ["plan.cpp", "abi.cpp", "sched.cpp", "attn_fwd.hip", "attn_bwd.hip", "lse_merge.hip", "layout.hip", "gate.hip", "rope.hip",
-           "linear_plan.cpp", "linear.hip"]
+           "linear_plan.cpp", "linear.hip", "norm.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

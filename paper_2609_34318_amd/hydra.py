@@ -75,6 +75,16 @@ class LinearC(ctypes.Structure):
                 ("v_tok_stride", ctypes.c_int32)]
 
 
+class NormC(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32),
+                ("d", ctypes.c_int32),
+                ("cp_u", ctypes.c_int32),
+                ("center", ctypes.c_int32),
+                ("activation", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
 class SchedConfig(ctypes.Structure):
     _fields_ = [("n_ranks", ctypes.c_int32),
                 ("token_budget", ctypes.c_int64),
@@ -210,6 +220,13 @@ def lib() -> ctypes.CDLL:
         L.hydra_linear_step.argtypes = [i32] * 6 + [ctypes.c_float] + [vp] * 9
         for name in ("hydra_linear_plan", "hydra_linear_fwd", "hydra_linear_bwd", "hydra_linear_step"):
             getattr(L, name).restype = ctypes.c_int
+        M = ctypes.POINTER(NormC)
+        L.hydra_norm_workspace_size.argtypes = [i64, i32, i32]
+        L.hydra_norm_workspace_size.restype = sz
+        L.hydra_unpack_heads_normed.argtypes = [M] + [vp] * 6
+        L.hydra_unpack_heads_normed.restype = ctypes.c_int
+        L.hydra_pack_heads_normed_bwd.argtypes = [M] + [vp] * 10 + [sz, vp]
+        L.hydra_pack_heads_normed_bwd.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -574,6 +591,48 @@ def pack_heads_gated_bwd(y, gate, d_y, d_send, d_gate, stream=None):
            "hydra_pack_heads_gated_bwd")
 
 
+# ------------------------------------------------------------------ head norm
+
+ACTIVATIONS = ("sigmoid", "silu")
+
+
+def norm_workspace_size(n_tokens: int, n_heads: int, d: int) -> int:
+    return int(lib().hydra_norm_workspace_size(n_tokens, n_heads, d))
+
+
+def _norm(x, weight, bias, gate, center: bool, activation: str, eps: float):
+    """The problem and the addresses of what both calls take, x [cp_u, T, H / cp_u, d]."""
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation {activation!r}: one of {ACTIVATIONS} is required")
+    cp_u, T, Hg, d = x.shape
+    H, n = cp_u * Hg, x.numel()
+    p = NormC(n_tokens=T, n_heads=H, d=d, cp_u=cp_u, center=int(bool(center)), activation=ACTIVATIONS.index(activation), eps=eps)
+    return ctypes.byref(p), n, H * d, (_ptr(x, "x", _BF16), _ptr(weight, "weight", _F32, H * d), _ptr(bias, "bias", _F32, H * d),
+                                       _ptr(gate, "gate", _BF16, n))
+
+
+def unpack_heads_normed(x, y, weight=None, bias=None, gate=None, center=True, activation="silu", eps: float = 1e-5,
+                        stream=None):
+    """x [cp_u, T, H/cp_u, d] bf16 -> y [T, H, d] bf16: every head normalised (center: its mean taken off), times weight
+    plus bias [H, d] float32, times activation(gate), gate logits [T, H, d] bf16; without a gate, activation of that."""
+    _here(x, y, weight, bias, gate)
+    p, n, _, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    _check(lib().hydra_unpack_heads_normed(p, *ins, _ptr(y, "y", _BF16, n), _stream(stream)), "hydra_unpack_heads_normed")
+
+
+def pack_heads_normed_bwd(x, d_y, d_x, weight=None, bias=None, gate=None, d_gate=None, d_weight=None, d_bias=None,
+                          workspace=None, center=True, activation="silu", eps: float = 1e-5, stream=None):
+    """Backward of unpack_heads_normed from its inputs and d_y [T, H, d] bf16: writes d_x (as x), with a gate d_gate, and
+    where given d_weight and d_bias [H, d] float32, for which workspace is a uint8 device tensor of
+    norm_workspace_size(T, H, d)."""
+    _here(x, d_y, d_x, weight, bias, gate, d_gate, d_weight, d_bias, workspace)
+    p, n, cols, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    _check(lib().hydra_pack_heads_normed_bwd(p, *ins, _ptr(d_y, "d_y", _BF16, n), _ptr(d_x, "d_x", _BF16, n),
+                                             _ptr(d_gate, "d_gate", _BF16, n), _ptr(d_weight, "d_weight", _F32, cols),
+                                             _ptr(d_bias, "d_bias", _F32, cols), *_scratch(workspace), _stream(stream)),
+           "hydra_pack_heads_normed_bwd")
+
+
 # ------------------------------------------------------------------ rotary positions
 
 class Rope:
@@ -866,12 +925,12 @@ def profile_start():
 
 def profile_stop() -> dict:
     """Stop timing; returns {kernel: {launches, total_ms, min_ms, max_ms, avg_ms}}."""
-    buf = (KernelStat * 32)()
-    n = lib().hydra_profile_stop(buf, 32)
+    buf = (KernelStat * 64)()
+    n = lib().hydra_profile_stop(buf, 64)
     if n < 0:
         raise HydraError(n, "hydra_profile_stop")
     out = {}
-    for i in range(min(n, 32)):
+    for i in range(min(n, 64)):
         k = buf[i]
         out[k.name.decode()] = dict(launches=k.launches, total_ms=k.total_ms, min_ms=k.min_ms,
                                     max_ms=k.max_ms, avg_ms=k.total_ms / max(k.launches, 1))
