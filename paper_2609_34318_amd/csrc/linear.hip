@@ -61,18 +61,38 @@ __device__ __forceinline__ float log2_decay(const float* decay, int head) {
   return fmax2(__int_as_float(((cint*)decay)[head]) * LOG2E, -1.0e30f);
 }
 
-// x as bf16, and what that leaves of it
-__device__ __forceinline__ void split_bf16(const float (&x)[8], bf16x8& hi, float (&rest)[8]) {
-  hi = to_bf16x8(x);
+// x as bf16, and what that leaves of it (the pairs' bits, so that a value is converted once)
+__device__ __forceinline__ bf16x8 split_bf16(float (&x)[8]) {
+  const bf16x8 hi = to_bf16x8(x);
+  const u32x4 bits = __builtin_bit_cast(u32x4, hi);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e] - (float)hi[e];
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] -= __uint_as_float(bits[i] << 16);
+    x[2 * i + 1] -= __uint_as_float(bits[i] & 0xffff0000u);
+  }
+  return hi;
 }
 
 template <int DA, int DC, bool MAIN> struct LinGeom {
   static constexpr int WAVES = DC / 32, COPY = WAVES >= 4 ? 4 : 2;  // waves that issue copies
   static constexpr int A = MAIN ? LB * DA * 2 : 0, B = LB * DA * 2, C = LB * DC * 2, STAGE = A + B + C;
-  static constexpr int LDS = 2 * STAGE;
+  // chunks in LDS, all but one of them on their way: two workgroups run on a CU, with half of its 160 KB each
+  static constexpr int STAGES = 4 * STAGE <= 80 << 10 ? 4 : 3 * STAGE <= 80 << 10 ? 3 : 2;
+  static constexpr int LDS = STAGES * STAGE;
+  static constexpr int COPIES = LB / 8 / COPY * (DA / 64 * (MAIN ? 2 : 1) + DC / 64);  // instructions of a copying wave
 };
+
+// Waits for all but the last N vector memory instructions of the wave.
+template <int N> __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// ... of a chunk's copies behind which STAGES - 2 chunks of `copies` are on their way, and the stores of the last T
+// chunks' rows (T up to STAGES - 1)
+template <int STAGES, int COPIES, int STORES> __device__ __forceinline__ void wait_chunk(int t) {
+  constexpr int N = (STAGES - 2) * COPIES;
+  if (STORES == 0 || t == 0) wait_vm<N>();
+  else if (STAGES == 2 || t == 1) wait_vm<N + STORES>();
+  else if (STAGES == 3 || t == 2) wait_vm<N + 2 * STORES>();
+  else wait_vm<N + 3 * STORES>();
+}
 
 // The lane's part of a 32-column state [DA][32] in the caller's layout.
 template <int DA, int DC, class F> __device__ __forceinline__ void each_state(float* p, int trans, int wave, int lane, F&& f) {
@@ -86,7 +106,8 @@ template <int DA, int DC, class F> __device__ __forceinline__ void each_state(fl
     }
 }
 
-template <int DA, int DC, bool REV, bool MAIN>
+// PARTS: bf16 values that a weighted c is cut into.  REST: X and S enter the products for y as two.
+template <int DA, int DC, bool REV, bool MAIN, int PARTS, bool REST>
 __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int item, int head, lds_char* smem) {
   typedef LinGeom<DA, DC, MAIN> G;
   constexpr int NB = DA / 32;
@@ -113,7 +134,7 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
     if (wave >= G::COPY) return;
     const int r = chunk_row(t), n = min(LB, rows - r);
     const int64_t row = row0 + r;
-    lds_char* s = smem + (t & 1) * G::STAGE;
+    lds_char* s = smem + (t % G::STAGES) * G::STAGE;
     if constexpr (MAIN) dma_tile<DA, LB, G::COPY>(s, tile_rsrc(w.a, row, n, w.a_s), a_off, w.a_s, wave);
     dma_tile<DA, LB, G::COPY>(s + G::A, tile_rsrc(w.b, row, n, w.b_s), b_off, w.b_s, wave);
     dma_tile<DC, LB, G::COPY>(s + G::A + G::B, tile_rsrc(w.c, row, n, w.c_s), c_off, w.c_s, wave);
@@ -154,7 +175,7 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
 #pragma unroll
   for (int b = 0; b < NB; ++b) settle(S[b]);
 
-  // weights: of X at this lane's element r, of the row of y, of c at this lane's rows
+  // weights: of X at this lane's element r, of c at this lane's rows
   float wx[16], wu[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
@@ -163,7 +184,6 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
     wu[r] = w.tu * power(float(REV ? j + 1 : LB - 1 - j));
   }
   const float full_decay = power(float(LB));
-  const bool three = w.out != nullptr;  // uniform
 
   OperandOffsets o = operand_offsets(lane);
   int nat[4];  // as o.b128, of row m
@@ -185,161 +205,200 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
   const int ct0 = (wave >> 1) * block_bytes<LB>() + ((wave & 1) ? o.tr[0][1] : o.tr[0][0]);
   const int ct1 = (wave >> 1) * block_bytes<LB>() + ((wave & 1) ? o.tr[1][1] : o.tr[1][0]);
 
-  if (n_chunks > 0) issue(0);
+#pragma unroll
+  for (int t = 0; t < G::STAGES - 1; ++t)
+    if (t < n_chunks) issue(t);
+  float unit = 1.f;
   for (int t = 0; t < n_chunks; ++t) {
     const int r0 = chunk_row(t), n = min(LB, rows - r0);
-    lds_char* As = smem + (t & 1) * G::STAGE;
+    lds_char* As = smem + (t % G::STAGES) * G::STAGE;
     lds_char* Bs = As + G::A;
     lds_char* Cs = Bs + G::B;
-    // this chunk's copies; the stores of the last one's rows, issued behind them, may be in flight
-    if (t == 0 || !want_y) wait_dma();
-    else if (w.y) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    // this chunk's copies; later ones' and the stores of earlier rows may be in flight
+    if (t + G::STAGES - 2 >= n_chunks) wait_dma();
+    else if (!want_y) wait_chunk<G::STAGES, G::COPIES, 0>(t);
+    else if (w.y) wait_chunk<G::STAGES, G::COPIES, 2>(t);
+    else wait_chunk<G::STAGES, G::COPIES, 4>(t);
     if (n < LB && wave < G::COPY) {
       clear_tail<DA, LB, G::COPY>(Bs, n, wave, lane);
       clear_tail<DC, LB, G::COPY>(Cs, n, wave, lane);
     }
     barrier_lds();
-    if (t + 1 < n_chunks) issue(t + 1);
+    if (t + G::STAGES - 1 < n_chunks) issue(t + G::STAGES - 1);
 
+    if (!REV && n < LB) {  // an item's last rows
+#pragma unroll
+      for (int r = 0; r < 16; ++r) wu[r] = w.tu * power(float(max(n - 1 - (16 * (r >> 3) + 8 * h + (r & 7)), 0)));
+      asm volatile("" ::: "memory");  // a branch: the compiler would compute both for every chunk
+    }
+    // S = unit S' of the registers: `unit` alone decays, and S' takes it up only where it leaves 2^-24 .. 2^24
+    const float unit0 = unit;
+    unit *= n == LB ? full_decay : power(float(n));
+    const bool rescale = __builtin_amdgcn_ballot_w64(!(unit > 0x1p-24f && unit < 0x1p24f)) != 0;
+    const float new_unit = rescale ? 1.f : unit, per_unit = __builtin_amdgcn_rcpf(new_unit);
+
+    // One block without branches, so that the vector work and the reads lie between the products.
     bf16x8 cf[2];  // c^T: lane = column, rows 16 s + 8 h .. + 7
 #pragma unroll
     for (int s = 0; s < 2; ++s) cf[s] = join(lds_tr8(Cs + 2048 * s + ct0), lds_tr8(Cs + 2048 * s + ct1));
-
-    if (want_y) {
-      f32x16 x = f32x16{}, y = f32x16{};
+    f32x16 x = f32x16{}, y = f32x16{};
+    if constexpr (MAIN) {
 #pragma unroll
       for (int k = 0; k < DA / 16; ++k) {
         const bf16x8 af = lds_ld16(As, nat[k & 3] + (k >> 2) * block_bytes<LB>());
         x = mfma(op_b128<LB>(Bs, o, 0, k), af, x);
-        float s8[8], rest[8];
+        float s8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) s8[e] = S[k >> 1][8 * (k & 1) + e];
-        bf16x8 hi;
-        split_bf16(s8, hi, rest);
-        y = mfma(hi, af, y);
-        y = mfma(to_bf16x8(rest), af, y);
+        if constexpr (!REST) {
+          y = mfma(to_bf16x8(s8), af, y);
+        } else {
+          y = mfma(split_bf16(s8), af, y);
+          y = mfma(to_bf16x8(s8), af, y);
+        }
       }
-      y *= w.ts * power(float(REV ? n - 1 - m : m + 1));
+    }
+    bf16x8 part[2][PARTS];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float c8[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c8[e] = (float)cf[s][e] * (wu[8 * s + e] * per_unit);
+#pragma unroll
+      for (int i = 0; i < PARTS - 1; ++i) part[s][i] = split_bf16(c8);
+      part[s][PARTS - 1] = to_bf16x8(c8);
+    }
+    if (rescale) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) S[b] *= unit;
+      asm volatile("" ::: "memory");
+    }
+    unit = new_unit;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const lds_char* q = Bs + (b >> 1) * block_bytes<LB>() + 2048 * s;
+        const bf16x8 bf = join(lds_tr8(q + trp[0][b & 1]), lds_tr8(q + trp[1][b & 1]));
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) S[b] = mfma(bf, part[s][i], S[b]);
+      }
+
+    if (want_y) {
+      y *= w.ts * unit0 * power(float(REV ? n - 1 - m : m + 1));
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        float p[8], rest[8];
+        float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = x[8 * s + e] * wx[8 * s + e];
-        bf16x8 hi;
-        split_bf16(p, hi, rest);
-        y = mfma(cf[s], hi, y);
-        y = mfma(cf[s], to_bf16x8(rest), y);
+        if constexpr (REST) y = mfma(cf[s], split_bf16(p), y);
+        y = mfma(cf[s], to_bf16x8(p), y);
       }
-      // rows out through c's tile, which every wave has read
-      barrier_lds();
+      // rows out through the wave's own columns of c's tile, which no other wave reads: 64 bytes of each row
       const int pitch = cm.H * DC;
-      const int64_t at = ((int64_t)(row0 + r0) * cm.H + head) * DC;
+      const int64_t at = ((int64_t)(row0 + r0) * cm.H + head) * DC + 32 * wave;
+      auto own = [&](int row, int chunk) {
+        return Cs + (wave >> 1) * block_bytes<LB>() + row * 128 + (((4 * (wave & 1) + chunk) ^ swz(row)) << 4);
+      };
+      wave_lds_order();
       if (w.y) {
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr)
-          *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(Cs + m * (DC * 2) + (((4 * wave + rr) ^ (m & 7)) << 4) + 8 * h) =
+          *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(own(m, rr) + 8 * h) =
               u32x2{pack_bf16x2(y[4 * rr], y[4 * rr + 1]), pack_bf16x2(y[4 * rr + 2], y[4 * rr + 3])};
-        barrier_lds();
+        wave_lds_order();
         const rows_rsrc ry = rows_buffer(w.y + at, n, pitch * 2);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int idx = tid + 2 * DC * i, row = idx / (DC / 8), ch = idx % (DC / 8);
-          const u32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(Cs + row * (DC * 2) + ((ch ^ (row & 7)) << 4));
-          __builtin_amdgcn_raw_buffer_store_b128(v, ry, row * pitch * 2 + ch * 16, 0, 0);
+          const int row = 16 * i + (lane >> 2), ch = lane & 3;
+          __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(own(row, ch)), ry,
+                                                 row * pitch * 2 + ch * 16, 0, 0);
         }
-      } else {  // 32 bits: 16 rows at a time
+      } else {  // 32 bits: 16 rows at a time, a row in two rows' places
         const rows_rsrc ry = rows_buffer(w.y32 + at, n, pitch * 4);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           if ((m >> 4) == half) {
 #pragma unroll
             for (int rr = 0; rr < 4; ++rr)
-              *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(Cs + (m & 15) * (DC * 4) + (((8 * wave + 2 * rr + h) ^ (m & 7)) << 4)) =
+              *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(own(2 * (m & 15) + (rr >> 1), 2 * (rr & 1) + h)) =
                   f32x4{y[4 * rr], y[4 * rr + 1], y[4 * rr + 2], y[4 * rr + 3]};
           }
-          barrier_lds();
+          wave_lds_order();
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int idx = tid + 2 * DC * i, row = idx / (DC / 4), ch = idx % (DC / 4);
-            const u32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(Cs + row * (DC * 4) + ((ch ^ (row & 7)) << 4));
-            __builtin_amdgcn_raw_buffer_store_b128(v, ry, (16 * half + row) * pitch * 4 + ch * 16, 0, 0);
+            const int row = 8 * i + (lane >> 3), ch = lane & 7;
+            __builtin_amdgcn_raw_buffer_store_b128(
+                *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(own(2 * row + (ch >> 2), ch & 3)), ry,
+                (16 * half + row) * pitch * 4 + ch * 16, 0, 0);
           }
-          if (half == 0) barrier_lds();
+          wave_lds_order();
         }
       }
     }
 
-    // S = L^n S + b^T (weighted c)
-    const float dec = n == LB ? full_decay : power(float(n));
-#pragma unroll
-    for (int b = 0; b < NB; ++b) S[b] *= dec;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float c8[8], rest[8], rest2[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float u = wu[8 * s + e];
-        if (!REV && n < LB) u = w.tu * power(float(max(n - 1 - (16 * s + 8 * h + e), 0)));
-        c8[e] = (float)cf[s][e] * u;
-      }
-      bf16x8 part[3];
-      split_bf16(c8, part[0], rest);
-      split_bf16(rest, part[1], rest2);
-      part[2] = to_bf16x8(rest2);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const lds_char* q = Bs + (b >> 1) * block_bytes<LB>() + 2048 * s;
-        const bf16x8 bf = join(lds_tr8(q + trp[0][b & 1]), lds_tr8(q + trp[1][b & 1]));
-        S[b] = mfma(bf, part[0], S[b]);
-        S[b] = mfma(bf, part[1], S[b]);
-        if (three) S[b] = mfma(bf, part[2], S[b]);
-      }
-    }
   }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) S[b] *= unit;
 
   if (!MAIN) store_slot(REV ? slot - 1 : slot + 1);
   else if (last && w.out)
     each_state<DA, DC>(w.out + user, w.trans, wave, lane, [&](int b, int r, float* p) { *p = S[b][r]; });
 }
 
-template <int DK, int DV, bool MAIN>
-__global__ __launch_bounds__(2 * DV) void lin_fwd_kernel(Walk w, Common cm) {
+template <int DK, int DV, bool MAIN, int PARTS>
+__global__ __launch_bounds__(2 * DV) __attribute__((amdgpu_waves_per_eu(2))) void lin_fwd_kernel(Walk w, Common cm) {
   __shared__ __attribute__((aligned(1024))) char smem[LinGeom<DK, DV, MAIN>::LDS];
-  lin_walk<DK, DV, false, MAIN>(w, cm, blockIdx.x / cm.H, blockIdx.x % cm.H, (lds_char*)smem);
+  lin_walk<DK, DV, false, MAIN, PARTS, true>(w, cm, blockIdx.x / cm.H, blockIdx.x % cm.H, (lds_char*)smem);
 }
 
 // The three walks of an item and head run on one XCD (workgroup b runs on XCD b % 8), one after another, and find each
-// other's tiles in its L2.
-template <int DK, int DV, bool MAIN>
-__global__ __launch_bounds__(2 * (DK > DV ? DK : DV)) void lin_bwd_kernel(Walk dq, Walk dk, Walk dv, Common cm) {
+// other's tiles in its L2.  The first launch has two: dk starts from the states of dv, transposed.
+template <int DK, int DV, bool MAIN, int PARTS>
+__global__ __launch_bounds__(2 * (DK > DV ? DK : DV)) __attribute__((amdgpu_waves_per_eu(2))) void lin_bwd_kernel(Walk dq, Walk dk, Walk dv, Common cm) {
   constexpr int L0 = LinGeom<DV, DK, MAIN>::LDS, L1 = LinGeom<DK, DV, MAIN>::LDS;
   __shared__ __attribute__((aligned(1024))) char smem[L0 > L1 ? L0 : L1];
-  const int j = blockIdx.x / N_XCD, role = j % 3, unit = j / 3 * N_XCD + blockIdx.x % N_XCD;
+  constexpr int ROLES = MAIN ? 3 : 2;
+  const int j = blockIdx.x / N_XCD, role = j % ROLES, unit = j / ROLES * N_XCD + blockIdx.x % N_XCD;
   const int item = unit / cm.H, head = unit % cm.H;
   if (item >= cm.n_items) return;
-  if (role == 0) lin_walk<DV, DK, false, MAIN>(dq, cm, item, head, (lds_char*)smem);
-  else if (role == 1) lin_walk<DV, DK, true, MAIN>(dk, cm, item, head, (lds_char*)smem);
-  else lin_walk<DK, DV, true, MAIN>(dv, cm, item, head, (lds_char*)smem);
+  if (role == 0) lin_walk<DV, DK, false, MAIN, 2, false>(dq, cm, item, head, (lds_char*)smem);
+  else if (role == 1) lin_walk<DK, DV, true, MAIN, PARTS, false>(dv, cm, item, head, (lds_char*)smem);
+  else if constexpr (MAIN) lin_walk<DV, DK, true, MAIN, 2, false>(dk, cm, item, head, (lds_char*)smem);
 }
 
 // The states that a cut sequence's items start from, out of what each adds: in order slot s = L^seg slot (s - 1) +
 // slot s from the third on (the first holds the start and the second the state behind the first item), from the end
-// the same backwards.  One lane walks four elements; eight slots' loads are in flight.
+// the same backwards.  One lane walks four elements; eight slots' loads are in flight.  turned: dk walks from the
+// transposed states of dv's walk, which are written as it loads them: a block of 32 x 32 is one of 4 KB in both.
 struct Scan {
-  float* slots;
+  float *slots, *turned;
   int rev;
 };
-__global__ __launch_bounds__(256) void lin_scan_kernel(Scan s0, Scan s1, Scan s2, const int* scans, Common cm, int seg, int dd) {
-  const Scan s = blockIdx.z == 0 ? s0 : blockIdx.z == 1 ? s1 : s2;
-  const int scan = blockIdx.y / cm.H, head = blockIdx.y % cm.H;
+__global__ __launch_bounds__(256) void lin_scan_kernel(Scan s0, Scan s1, const int* scans, Common cm, int seg, int dk, int dv) {
+  const Scan s = blockIdx.z == 0 ? s0 : s1;
+  const int scan = blockIdx.y / cm.H, head = blockIdx.y % cm.H, dd = dk * dv;
   const int slot0 = scans[2 * scan], n = scans[2 * scan + 1];
   const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (e >= dd) return;
   const float decay = __builtin_amdgcn_exp2f(log2_decay(cm.decay, head) * float(seg));
   const int64_t step = (int64_t)cm.H * dd * (s.rev ? -1 : 1);
-  float* p = s.slots + ((int64_t)(s.rev ? slot0 + n - 1 : slot0) * cm.H + head) * dd + e;
+  const int64_t at = ((int64_t)(s.rev ? slot0 + n - 1 : slot0) * cm.H + head) * dd;
+  float* p = s.slots + at + e;
+  // element (row of dk, column of dv) = (16 (rr / 2) + 8 h + 4 (rr % 2) + 0 .. 3, m) of block (b, w)
+  const int w = e / (dk * 32), b = e / 1024 % (dk / 32), rr = e / 256 % 4, lane = e / 4 % 64, m = lane & 31, h = lane >> 5;
+  const int row = 16 * (rr >> 1) + 8 * h + 4 * (rr & 1);
+  float* q = s.turned ? s.turned + at + b * (dv * 32) + (4 * w + 2 * (m >> 4) + ((m >> 2) & 1)) * 256 +
+                            (32 * ((m >> 3) & 1) + row) * 4 + (m & 3)
+                      : nullptr;
+  auto turn = [&](int i, f32x4 v) {
+    if (!q) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) q[i * step + 4 * t] = v[t];
+  };
   f32x4 v = *reinterpret_cast<const f32x4*>(p + step);
+  turn(0, *reinterpret_cast<const f32x4*>(p));
+  turn(1, v);
   constexpr int AHEAD = 8;
   for (int i = 2; i < n; i += AHEAD) {
     f32x4 u[AHEAD];
@@ -351,22 +410,32 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(Scan s0, Scan s1, Scan s2
       if (i + k < n) {
         v = v * decay + u[k];
         *reinterpret_cast<f32x4*>(p + (i + k) * step) = v;
+        turn(i + k, v);
       }
   }
 }
 
-// Sums over the query heads of a K/V head: x [rows][Hkv][grp][d] in 32 bits -> y [rows][Hkv][d] bf16.
-__global__ __launch_bounds__(256) void lin_group_kernel(const float* __restrict__ x, uint16_t* __restrict__ y, int64_t n8,
-                                                        int d8, int grp) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
-    const float* p = x + (i / d8 * grp * d8 + i % d8) * 8;
+// Sums over the query heads of a K/V head: x [rows][Hkv][grp][8 d8] in 32 bits -> y [rows][Hkv][8 d8] bf16, n8 pieces of
+// eight; dk, then dv.
+struct Group {
+  const float* x;
+  uint16_t* y;
+  int64_t n8;
+  int d8;
+};
+__global__ __launch_bounds__(256) void lin_group_kernel(Group k, Group v, int grp) {
+  for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < k.n8 + v.n8; j += (int64_t)gridDim.x * 256) {
+    const bool second = j >= k.n8;
+    const int64_t i = second ? j - k.n8 : j;
+    const int d8 = second ? v.d8 : k.d8;
+    const float* p = (second ? v.x : k.x) + (i / d8 * grp * d8 + i % d8) * 8;
     f32x4 lo = f32x4{}, hi = f32x4{};
     for (int g = 0; g < grp; ++g, p += d8 * 8) {
       lo += *reinterpret_cast<const f32x4*>(p);
       hi += *reinterpret_cast<const f32x4*>(p + 4);
     }
-    const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    *reinterpret_cast<bf16x8*>(y + i * 8) = to_bf16x8(v);
+    const float r[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    *reinterpret_cast<bf16x8*>((second ? v.y : k.y) + i * 8) = to_bf16x8(r);
   }
 }
 
@@ -487,61 +556,76 @@ uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t width) {
   return rows > 0 ? uint64_t((rows - 1) * stride + width) * 2 : 0;
 }
 
-// What a plan depends on; the leading number is no head count of an attention plan's.
-std::vector<int64_t> linear_key(const LinearProblem& pr) {
-  std::vector<int64_t> k = {-2, pr.H};
-  k.insert(k.end(), pr.cu.begin(), pr.cu.end());
-  return k;
-}
-
-int upload(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, void* ws, hipStream_t s) {
-  std::vector<int32_t> image(w.slots_off / sizeof(int32_t), 0);
-  std::copy(plan.items.begin(), plan.items.end(), image.begin() + int64_t(w.items_off / sizeof(int32_t)));
-  std::copy(plan.scans.begin(), plan.scans.end(), image.begin() + int64_t(w.scans_off / sizeof(int32_t)));
-  // pageable source: the runtime has consumed the image when the call returns
-  if (!image.empty() &&
-      hipMemcpyAsync(ws, image.data(), image.size() * sizeof(int32_t), hipMemcpyHostToDevice, s) != hipSuccess)
-    return HYDRA_ERR_HIP;
-  plans_record(ws, linear_key(pr));
-  return HYDRA_OK;
-}
-
-// The workspace checked and holding the plan.
-int ready(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, bool planned, void* ws, size_t bytes,
-          hipStream_t s) {
-  if (!planned) return upload(pr, plan, w, ws, s);
-  return plans_hold(ws, linear_key(pr)) ? HYDRA_OK : HYDRA_ERR_WORKSPACE;
-}
-
-hipError_t scan(const LinearProblem& pr, const LinearPlan& plan, const LinearLayout& w, char* ws, const Common& cm,
-                std::initializer_list<Scan> walks, hipStream_t s) {
-  const Scan* p = walks.begin();
-  const int n = int(walks.size()), dd = pr.dk * pr.dv;
-  Timed timed("linear_scan", s);
-  // a grid's second size ends at 65535
-  const int per = std::max(1, 65535 / pr.H);
-  for (int at = 0; at < plan.n_scans; at += per)
-    hipLaunchKernelGGL(lin_scan_kernel, dim3(unsigned(dd + 1023) / 1024, unsigned(std::min(per, plan.n_scans - at) * pr.H), unsigned(n)),
-                       dim3(256), 0, s, p[0], p[n > 1 ? 1 : 0], p[n > 2 ? 2 : 0],
-                       reinterpret_cast<const int*>(ws + w.scans_off) + 2 * at, cm, plan.seg, dd);
-  return hipGetLastError();
-}
+// A checked problem, its plans and its workspace.
+struct Plans {
+  LinearProblem pr;
+  LinearPlan plan[2];  // LinearFor
+  LinearLayout w;
+  int make(const hydra_linear_t* p) {
+    if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+    linear_plan(pr, LinearFor::kForward, &plan[0]);
+    linear_plan(pr, LinearFor::kBackward, &plan[1]);
+    w = linear_layout(pr, plan[0], plan[1]);
+    return HYDRA_OK;
+  }
+  int check_workspace(const void* ws, size_t bytes) const {
+    if (!ws || bytes < w.total) return HYDRA_ERR_WORKSPACE;
+    return misaligned(ws, 16) ? HYDRA_ERR_ALIGN : HYDRA_OK;
+  }
+  // What a plan depends on; the leading number is no head count of an attention plan's.
+  std::vector<int64_t> key() const {
+    std::vector<int64_t> k = {-2, pr.H};
+    k.insert(k.end(), pr.cu.begin(), pr.cu.end());
+    return k;
+  }
+  int upload(void* ws, hipStream_t s) const {
+    std::vector<int32_t> image(w.slots_off / sizeof(int32_t), 0);
+    for (int i = 0; i < 2; ++i) {
+      std::copy(plan[i].items.begin(), plan[i].items.end(), image.begin() + int64_t(w.items_off[i] / sizeof(int32_t)));
+      std::copy(plan[i].scans.begin(), plan[i].scans.end(), image.begin() + int64_t(w.scans_off[i] / sizeof(int32_t)));
+    }
+    // pageable source: the runtime has consumed the image when the call returns
+    if (hipMemcpyAsync(ws, image.data(), image.size() * sizeof(int32_t), hipMemcpyHostToDevice, s) != hipSuccess)
+      return HYDRA_ERR_HIP;
+    plans_record(ws, key());
+    return HYDRA_OK;
+  }
+  // The workspace holds the plan.
+  int ready(bool planned, void* ws, hipStream_t s) const {
+    if (!planned) return upload(ws, s);
+    return plans_hold(ws, key()) ? HYDRA_OK : HYDRA_ERR_WORKSPACE;
+  }
+  Common common(LinearFor call, const void* ws, const float* decay) const {
+    const int i = int(call);
+    return {reinterpret_cast<const int*>(static_cast<const char*>(ws) + w.items_off[i]), decay, plan[i].n_items, pr.H};
+  }
+  hipError_t scan(LinearFor call, const char* ws, const Common& cm, std::initializer_list<Scan> walks, hipStream_t s) const {
+    const Scan* p = walks.begin();
+    const int n = int(walks.size()), i = int(call);
+    Timed timed("linear_scan", s);
+    // a grid's second size ends at 65535
+    const int per = std::max(1, 65535 / pr.H);
+    for (int at = 0; at < plan[i].n_scans; at += per)
+      hipLaunchKernelGGL(lin_scan_kernel, dim3(unsigned(pr.dk * pr.dv / 1024), unsigned(std::min(per, plan[i].n_scans - at) * pr.H), unsigned(n)),
+                         dim3(256), 0, s, p[0], p[n > 1 ? 1 : 0], reinterpret_cast<const int*>(ws + w.scans_off[i]) + 2 * at, cm,
+                         plan[i].seg, pr.dk, pr.dv);
+    return hipGetLastError();
+  }
+};
 
 int linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
                const float* state_in, void* o, float* state_out, void* workspace, size_t bytes, bool planned, void* stream) {
-  LinearProblem pr;
-  if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+  Plans P;
+  if (int rc = P.make(p); rc != HYDRA_OK) return rc;
+  const LinearProblem& pr = P.pr;
+  const LinearLayout& w = P.w;
   const uint64_t states = uint64_t(pr.cu.size() - 1) * pr.H * pr.dk * pr.dv * 4;
   if (!decay) return HYDRA_ERR_INVALID;
   if (pr.rows > 0 && (!q || !k || !v || (!o && !state_out))) return HYDRA_ERR_INVALID;
   for (const void* x : {q, k, v, static_cast<const void*>(state_in), static_cast<const void*>(o), static_cast<const void*>(state_out)})
     if (misaligned(x, 16)) return HYDRA_ERR_ALIGN;
   if (misaligned(decay, 4)) return HYDRA_ERR_ALIGN;
-  LinearPlan plan;
-  linear_plan(pr, &plan);
-  const LinearLayout w = linear_layout(pr, plan);
-  if (!workspace || bytes < w.total) return HYDRA_ERR_WORKSPACE;
-  if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  if (int rc = P.check_workspace(workspace, bytes); rc != HYDRA_OK) return rc;
   const Span outs[3] = {{o, uint64_t(pr.rows) * pr.H * pr.dv * 2}, {state_out, states}, {workspace, w.total}};
   const Span qs{q, rows_bytes(pr.rows, pr.q_s, pr.H * pr.dk)}, ks{k, rows_bytes(pr.rows, pr.k_s, pr.Hkv * pr.dk)},
       vs{v, rows_bytes(pr.rows, pr.v_s, pr.Hkv * pr.dv)}, ds{decay, uint64_t(pr.H) * 4},
@@ -550,9 +634,10 @@ int linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void
     return HYDRA_ERR_INVALID;
   if (pr.rows == 0 && !state_out) return HYDRA_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (int rc = ready(pr, plan, w, planned, workspace, bytes, s); rc != HYDRA_OK) return rc;
+  if (int rc = P.ready(planned, workspace, s); rc != HYDRA_OK) return rc;
   char* ws = static_cast<char*>(workspace);
-  const Common cm{reinterpret_cast<const int*>(ws + w.items_off), decay, plan.n_items, pr.H};
+  const LinearPlan& plan = P.plan[int(LinearFor::kForward)];
+  const Common cm = P.common(LinearFor::kForward, ws, decay);
   const int grp = pr.H / pr.Hkv;
   auto u16 = [](const void* x) { return static_cast<const uint16_t*>(x); };
   const Walk walk{u16(q), u16(k), u16(v), pr.q_s, pr.k_s, pr.v_s, 1, grp, grp, state_in, state_out,
@@ -562,12 +647,14 @@ int linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void
     if (plan.n_split > 0) {
       {
         Timed timed("linear_states", s);
-        hipLaunchKernelGGL((lin_fwd_kernel<DK, DV, false>), dim3(unsigned(plan.n_split) * pr.H), dim3(2 * DV), 0, s, walk, cm);
+        const auto kernel = state_out ? lin_fwd_kernel<DK, DV, false, 3> : lin_fwd_kernel<DK, DV, false, 2>;
+        hipLaunchKernelGGL(kernel, dim3(unsigned(plan.n_split) * pr.H), dim3(2 * DV), 0, s, walk, cm);
       }
-      if (hipError_t x = scan(pr, plan, w, ws, cm, {Scan{walk.slots, 0}}, s); x != hipSuccess) return x;
+      if (hipError_t x = P.scan(LinearFor::kForward, ws, cm, {Scan{walk.slots, nullptr, 0}}, s); x != hipSuccess) return x;
     }
     Timed timed("linear_fwd", s);
-    hipLaunchKernelGGL((lin_fwd_kernel<DK, DV, true>), dim3(unsigned(plan.n_items) * pr.H), dim3(2 * DV), 0, s, walk, cm);
+    const auto kernel = state_out ? lin_fwd_kernel<DK, DV, true, 3> : lin_fwd_kernel<DK, DV, true, 2>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(plan.n_items) * pr.H), dim3(2 * DV), 0, s, walk, cm);
     return hipGetLastError();
   });
   return e == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
@@ -576,8 +663,10 @@ int linear_fwd(const hydra_linear_t* p, const void* q, const void* k, const void
 int linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void* v, const float* decay,
                const float* state_in, const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv,
                float* d_state_in, void* workspace, size_t bytes, bool planned, void* stream) {
-  LinearProblem pr;
-  if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
+  Plans P;
+  if (int rc = P.make(p); rc != HYDRA_OK) return rc;
+  const LinearProblem& pr = P.pr;
+  const LinearLayout& w = P.w;
   const uint64_t states = uint64_t(pr.cu.size() - 1) * pr.H * pr.dk * pr.dv * 4;
   if (!decay) return HYDRA_ERR_INVALID;
   if (pr.rows > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv)) return HYDRA_ERR_INVALID;
@@ -586,11 +675,7 @@ int linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void
                         static_cast<const void*>(d_state_in)})
     if (misaligned(x, 16)) return HYDRA_ERR_ALIGN;
   if (misaligned(decay, 4)) return HYDRA_ERR_ALIGN;
-  LinearPlan plan;
-  linear_plan(pr, &plan);
-  const LinearLayout w = linear_layout(pr, plan);
-  if (!workspace || bytes < w.total) return HYDRA_ERR_WORKSPACE;
-  if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
+  if (int rc = P.check_workspace(workspace, bytes); rc != HYDRA_OK) return rc;
   const uint64_t n = uint64_t(pr.rows);
   if (outputs_overlap({{dq, n * pr.H * pr.dk * 2}, {dk, n * pr.Hkv * pr.dk * 2}, {dv, n * pr.Hkv * pr.dv * 2},
                        {d_state_in, states}, {workspace, w.total}},
@@ -600,9 +685,10 @@ int linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void
     return HYDRA_ERR_INVALID;
   if (pr.rows == 0 && !d_state_in) return HYDRA_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (int rc = ready(pr, plan, w, planned, workspace, bytes, s); rc != HYDRA_OK) return rc;
+  if (int rc = P.ready(planned, workspace, s); rc != HYDRA_OK) return rc;
   char* ws = static_cast<char*>(workspace);
-  const Common cm{reinterpret_cast<const int*>(ws + w.items_off), decay, plan.n_items, pr.H};
+  const LinearPlan& plan = P.plan[int(LinearFor::kBackward)];
+  const Common cm = P.common(LinearFor::kBackward, ws, decay);
   const int grp = pr.H / pr.Hkv, dos = pr.H * pr.dv;
   const int64_t slots = int64_t(plan.n_split) * pr.H * pr.dk * pr.dv;
   float* at = reinterpret_cast<float*>(ws + w.slots_off);
@@ -617,31 +703,29 @@ int linear_bwd(const hydra_linear_t* p, const void* q, const void* k, const void
                 out16(dv), out32(w.dv_off), pr.scale, 1.f, pr.scale};
   const hipError_t e = with_dims(pr.dk, pr.dv, [&](auto dk_, auto dv_) {
     constexpr int DK = decltype(dk_)::value, DV = decltype(dv_)::value;
-    auto grid = [&](int items) { return dim3(unsigned((int64_t(items) * pr.H + N_XCD - 1) / N_XCD * N_XCD * 3)); };
+    auto grid = [&](int items, int walks) { return dim3(unsigned((int64_t(items) * pr.H + N_XCD - 1) / N_XCD * N_XCD * walks)); };
     const dim3 block(2 * std::max(DK, DV));
     if (plan.n_split > 0) {
       {
         Common first = cm;
         first.n_items = plan.n_split;
         Timed timed("linear_states", s);
-        hipLaunchKernelGGL((lin_bwd_kernel<DK, DV, false>), grid(plan.n_split), block, 0, s, wq, wk, wv, first);
+        const auto kernel = d_state_in ? lin_bwd_kernel<DK, DV, false, 3> : lin_bwd_kernel<DK, DV, false, 2>;
+        hipLaunchKernelGGL(kernel, grid(plan.n_split, 2), block, 0, s, wq, wk, wv, first);
       }
-      if (hipError_t x = scan(pr, plan, w, ws, cm, {Scan{wq.slots, 0}, Scan{wk.slots, 1}, Scan{wv.slots, 1}}, s); x != hipSuccess)
+      if (hipError_t x = P.scan(LinearFor::kBackward, ws, cm, {Scan{wq.slots, nullptr, 0}, Scan{wv.slots, wk.slots, 1}}, s); x != hipSuccess)
         return x;
     }
     {
       Timed timed("linear_bwd", s);
-      hipLaunchKernelGGL((lin_bwd_kernel<DK, DV, true>), grid(plan.n_items), block, 0, s, wq, wk, wv, cm);
+      const auto kernel = d_state_in ? lin_bwd_kernel<DK, DV, true, 3> : lin_bwd_kernel<DK, DV, true, 2>;
+      hipLaunchKernelGGL(kernel, grid(plan.n_items, 3), block, 0, s, wq, wk, wv, cm);
     }
     if (grp > 1 && pr.rows > 0) {
       Timed timed("linear_groups", s);
-      auto sum = [&](const float* x, void* y, int d) {
-        const int64_t n8 = pr.rows * pr.Hkv * d / 8;
-        hipLaunchKernelGGL(lin_group_kernel, dim3(unsigned(std::min<int64_t>((n8 + 255) / 256, 1 << 16))), dim3(256), 0, s, x,
-                           static_cast<uint16_t*>(y), n8, d / 8, grp);
-      };
-      sum(wk.y32, dk, DK);
-      sum(wv.y32, dv, DV);
+      const int64_t nk = pr.rows * pr.Hkv * DK / 8, nv = pr.rows * pr.Hkv * DV / 8;
+      hipLaunchKernelGGL(lin_group_kernel, dim3(unsigned(std::min<int64_t>((nk + nv + 255) / 256, 1 << 16))), dim3(256), 0, s,
+                         Group{wk.y32, static_cast<uint16_t*>(dk), nk, DK / 8}, Group{wv.y32, static_cast<uint16_t*>(dv), nv, DV / 8}, grp);
     }
     return hipGetLastError();
   });
@@ -657,11 +741,8 @@ extern "C" {
 
 size_t hydra_linear_workspace_size(const hydra_linear_t* p) {
   try {
-    LinearProblem pr;
-    if (check_linear(p, &pr) != HYDRA_OK) return 0;
-    LinearPlan plan;
-    linear_plan(pr, &plan);
-    return linear_layout(pr, plan).total;
+    Plans P;
+    return P.make(p) == HYDRA_OK ? P.w.total : 0;
   } catch (...) {
     return 0;
   }
@@ -669,14 +750,10 @@ size_t hydra_linear_workspace_size(const hydra_linear_t* p) {
 
 int hydra_linear_plan(const hydra_linear_t* p, void* workspace, size_t workspace_bytes, void* stream) {
   try {
-    LinearProblem pr;
-    if (int rc = check_linear(p, &pr); rc != HYDRA_OK) return rc;
-    LinearPlan plan;
-    linear_plan(pr, &plan);
-    const LinearLayout w = linear_layout(pr, plan);
-    if (!workspace || workspace_bytes < w.total) return HYDRA_ERR_WORKSPACE;
-    if (misaligned(workspace, 16)) return HYDRA_ERR_ALIGN;
-    return upload(pr, plan, w, workspace, static_cast<hipStream_t>(stream));
+    Plans P;
+    if (int rc = P.make(p); rc != HYDRA_OK) return rc;
+    if (int rc = P.check_workspace(workspace, workspace_bytes); rc != HYDRA_OK) return rc;
+    return P.upload(workspace, static_cast<hipStream_t>(stream));
   } catch (...) {
     return HYDRA_ERR_INVALID;
   }

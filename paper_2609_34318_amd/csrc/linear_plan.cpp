@@ -9,9 +9,12 @@ namespace hydra {
 namespace {
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Workgroups that a walk is cut into, and the fewest rows of an item of a cut sequence.
-constexpr int64_t kLinearGroups = 1024;
-constexpr int64_t kLinearMinRows = 256;
+// Workgroups that a walk is cut into: two run on each of 256 CUs.  The three walks of the backward make 1.5 times as
+// many of half the number, and its states and their scan cost more (16K rows x 16 heads of 128 x 128: forward 143 us in
+// 512 items, 164 in 336, 154 in 256; backward 284, 264, 249, and 243 in 170).
+constexpr int64_t kLinearGroups[2] = {512, 256};
+// The fewest rows of an item of a cut sequence (2K rows in four documents x 8 heads of 64 x 64: forward 26 us, 33 with 256).
+constexpr int64_t kLinearMinRows = 128;
 }  // namespace
 
 int check_linear(const hydra_linear_t* p, LinearProblem* out) {
@@ -45,15 +48,20 @@ int check_linear(const hydra_linear_t* p, LinearProblem* out) {
   out->cu.assign(p->cu_seqlens, p->cu_seqlens + size_t(p->n_seqs) + 1);
   out->rows = rows;
   // one workgroup per item and head, of three walks in the backward, in a dispatch of fewer than 2^32 lanes
-  LinearPlan plan;
-  linear_plan(*out, &plan);
-  if (int64_t(plan.n_items) * out->H >= (int64_t(1) << 21)) return HYDRA_ERR_INVALID;
+  const int64_t most = (rows * out->H + kLinearMinRows - 1) / kLinearMinRows + int64_t(p->n_seqs) * out->H;
+  if (most >= (int64_t(1) << 21)) {  // what the bound without the plan does not say
+    LinearPlan plan;
+    for (LinearFor call : {LinearFor::kForward, LinearFor::kBackward}) {
+      linear_plan(*out, call, &plan);
+      if (int64_t(plan.n_items) * out->H >= (int64_t(1) << 21)) return HYDRA_ERR_INVALID;
+    }
+  }
   return HYDRA_OK;
 }
 
-void linear_plan(const LinearProblem& pr, LinearPlan* out) {
+void linear_plan(const LinearProblem& pr, LinearFor call, LinearPlan* out) {
   *out = LinearPlan{};
-  const int64_t even = (pr.rows * pr.H + kLinearGroups - 1) / kLinearGroups;
+  const int64_t groups = kLinearGroups[int(call)], even = (pr.rows * pr.H + groups - 1) / groups;
   out->seg = int(std::max(kLinearMinRows, (even + 63) / 64 * 64));
   const int n_seqs = int(pr.cu.size()) - 1;
   std::vector<std::pair<int32_t, int>> whole;  // rows, sequence
@@ -78,7 +86,7 @@ void linear_plan(const LinearProblem& pr, LinearPlan* out) {
   for (const auto& w : whole) add(pr.cu[size_t(w.second)], w.first, w.second, true, true, -1);
 }
 
-LinearLayout linear_layout(const LinearProblem& pr, const LinearPlan& plan) {
+LinearLayout linear_layout(const LinearProblem& pr, const LinearPlan& fwd, const LinearPlan& bwd) {
   LinearLayout w{};
   size_t off = 0;
   auto take = [&](uint64_t bytes) {
@@ -86,9 +94,13 @@ LinearLayout linear_layout(const LinearProblem& pr, const LinearPlan& plan) {
     off = align_up(off + size_t(bytes), 256);
     return at;
   };
-  w.items_off = take(plan.items.size() * sizeof(int32_t));
-  w.scans_off = take(plan.scans.size() * sizeof(int32_t));
-  w.slots_off = take(uint64_t(plan.n_split) * uint64_t(pr.H) * uint64_t(pr.dk) * uint64_t(pr.dv) * 4 * 3);
+  for (int i = 0; i < 2; ++i) {
+    const LinearPlan& plan = i == 0 ? fwd : bwd;
+    w.items_off[i] = take(plan.items.size() * sizeof(int32_t));
+    w.scans_off[i] = take(plan.scans.size() * sizeof(int32_t));
+  }
+  const uint64_t slots = uint64_t(std::max(fwd.n_split, 3 * bwd.n_split));
+  w.slots_off = take(slots * uint64_t(pr.H) * uint64_t(pr.dk) * uint64_t(pr.dv) * 4);
   const uint64_t heads = pr.Hkv < pr.H ? uint64_t(pr.rows) * uint64_t(pr.H) : 0;
   w.dk_off = take(heads * uint64_t(pr.dk) * 4);
   w.dv_off = take(heads * uint64_t(pr.dv) * 4);

@@ -29,6 +29,8 @@ struct LinearProblem {
 };
 int check_linear(const hydra_linear_t* p, LinearProblem* out);
 
+// The forward and the backward cut long sequences at different lengths.
+enum class LinearFor { kForward, kBackward };
 // The items, those of sequences of several items first (n_split of them, each sequence's in order and in slots one
 // after another), the others by length; and of every such sequence {first slot, items}.
 struct LinearPlan {
@@ -36,13 +38,13 @@ struct LinearPlan {
   int n_items = 0, n_split = 0, n_scans = 0;
   std::vector<int32_t> items, scans;
 };
-void linear_plan(const LinearProblem& pr, LinearPlan* out);
+void linear_plan(const LinearProblem& pr, LinearFor call, LinearPlan* out);
 
-// Byte offsets of the workspace regions: the plan, the states of three walks (the forward has one), and for grouped
-// heads dk and dv of every query head in 32 bits.
+// Byte offsets of the workspace regions: the plans of both, the states of the walks of either (one of the forward, three
+// of the backward), and for grouped heads dk and dv of every query head in 32 bits.
 struct LinearLayout {
-  size_t items_off, scans_off, slots_off, dk_off, dv_off, total;
+  size_t items_off[2], scans_off[2], slots_off, dk_off, dv_off, total;
 };
-LinearLayout linear_layout(const LinearProblem& pr, const LinearPlan& plan);
+LinearLayout linear_layout(const LinearProblem& pr, const LinearPlan& fwd, const LinearPlan& bwd);
 
 }  // namespace hydra
