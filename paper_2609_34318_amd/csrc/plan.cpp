@@ -297,6 +297,8 @@ int64_t record_tiles(const Problem& pr, Kernel kernel, const int32_t* u) {
 
 }  // namespace
 
+bool uneven(const Problem& pr) { return pr.window > 0 && pr.sinks > 0; }
+
 Ahead launch_load(const Problem& pr, Kernel kernel, const std::vector<int32_t>& records, int heads, const UnitList& list) {
   Ahead a;
   const std::vector<int32_t>& units = list.units.empty() ? records : list.units;
@@ -317,7 +319,8 @@ void split_units(const Problem& pr, Kernel kernel, const std::vector<int32_t>& r
                  const Ahead& ahead) {
   *out = UnitList{};
   const int64_t n = int64_t(records.size()) / kUnitInts;
-  if (n == 0 || heads <= 0 || n * heads >= kSplitBelow) return;
+  const bool many = n * heads >= kSplitBelow;
+  if (n == 0 || heads <= 0 || (many && !(uneven(pr) && kernel == Kernel::kDkdv))) return;
   std::vector<int64_t> tiles(static_cast<size_t>(n));
   int64_t longest = 0;
   for (int64_t i = 0; i < n; ++i) {
@@ -365,7 +368,19 @@ void split_units(const Problem& pr, Kernel kernel, const std::vector<int32_t>& r
   };
   int64_t parts = 0, best_most = longest;
   double best = time_of(longest, &parts);
-  for (int d = 2; d <= 32; ++d) {
+  if (many) {
+    // The CUs are full, but an item must not outlast what runs beside it: a head's items on its XCD's 32 CUs where the
+    // heads come one after another (xcd_head_item), else all heads' on all.
+    const double all = double(std::accumulate(tiles.begin(), tiles.end(), int64_t(0))) + double(n) * cost.group;
+    const double beside = heads % 8 == 0 ? all / 32 : all * heads / kCus;
+    for (int64_t most = std::max<int64_t>(int64_t(0.75 * beside - cost.group), 2 * kMinPart); most < longest; most += (most + 3) / 4) {
+      time_of(most, &parts);
+      if (parts * heads > MAX_PARTS) continue;
+      best_most = most;
+      break;
+    }
+  }
+  for (int d = 2; d <= 32 && !many; ++d) {
     const int64_t most = (longest + d - 1) / d;
     if (most < kMinPart) break;
     const double t = time_of(most, &parts) + (ahead.merges ? 0 : cost.merge);
@@ -497,7 +512,8 @@ WsLayout ws_layout(const Problem& pr, bool noalloc) {
   w.qitems_off = off;
   off = align_up(off + size_t(nqt) * kUnitInts * sizeof(int32_t), 256);
   w.lists_off = off;
-  if (!noalloc) off += 3 * kListBytes;
+  if (!noalloc)  // what is uneven may be split beside more whole items
+    off += 3 * (kListBytes + (uneven(pr) ? align_up(size_t(std::max(nqt, nkt)) * kUnitInts * sizeof(int32_t), 256) : 0));
   w.d_off = off;
   off = align_up(off + size_t(pr.H) * size_t(pr.nq) * sizeof(float), 256);
   w.lse2_off = off;
@@ -571,7 +587,7 @@ uint64_t parts_bytes(Kernel kernel, const ListSize& l, int heads) {
 }
 
 uint64_t split_scratch_bytes(const Problem& pr) {
-  if (n_tiles(pr.q, kQTile) * pr.H >= kSplitBelow && n_tiles(pr.kv, kKvTile) * pr.Hkv >= kSplitBelow) return 0;
+  if (!uneven(pr) && n_tiles(pr.q, kQTile) * pr.H >= kSplitBelow && n_tiles(pr.kv, kKvTile) * pr.Hkv >= kSplitBelow) return 0;
   PlanImage img;
   plan_image(pr, ws_layout(pr), PlanFor::kBackward, true, &img);
   return std::max(parts_bytes(Kernel::kFwd, img.fwd, pr.H),

@@ -65,6 +65,9 @@ constexpr int kMaxMerges = MAX_PARTS / 2;  // a split item has at least two part
 // Workgroups of a launch from which on nothing is split: at two per CU (256) and more the
 // heavy-first order fills the chip, and no shape measured there gained.
 constexpr int64_t kSplitBelow = 512;
+// With a window the tile of keys that holds a document's sinks is seen by all of its queries and the others by few: its
+// items are split, however many the launch has, where the longest of them would take longer than all else over the CUs.
+bool uneven(const Problem& pr);
 // The most bytes of a split list: its merges, and a unit for every part and every whole item.
 constexpr size_t kListBytes = (size_t(kMaxMerges) * kMergeInts + size_t(MAX_PARTS + kSplitBelow) * kUnitInts) * sizeof(int32_t);
 static_assert(kListBytes % 256 == 0, "lists end on a region boundary");

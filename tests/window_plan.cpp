@@ -129,6 +129,60 @@ int main() {
       }
     }
   }
+  // launches of many items, one of which all queries see: its parts cover its tiles, the lists fit their place, and no part
+  // is longer than what a head's items take on an eighth of the CUs
+  int64_t split = 0;
+  for (int trial = 0; trial < 60; ++trial) {
+    const int heads[] = {1, 8, 16, 24, 64, 3};
+    std::vector<int32_t> cu{0};
+    for (int d = int(uni(1, 3)); d > 0; --d) cu.push_back(cu.back() + int32_t(uni(1, trial % 5 ? 30000 : 200000)));
+    hydra_problem_t p{};
+    p.n_heads = heads[trial % 6];
+    p.d_qk = 192;
+    p.d_v = 128;
+    p.cu_seqlens = cu.data();
+    p.n_docs = int32_t(cu.size()) - 1;
+    p.q.n_segs = p.kv.n_segs = 1;
+    p.q.len[0] = p.kv.len[0] = cu.back();
+    hydra_scores_t sc{};
+    sc.window = int32_t(uni(1, 6000));
+    sc.sinks = int32_t(uni(0, 3) * uni(1, 100));
+    Problem pr;
+    CHECK(check_problem(&p, &sc, &pr) == HYDRA_OK);
+    const WsLayout w = ws_layout(pr);
+    for (PlanFor call : {PlanFor::kForward, PlanFor::kBackward, PlanFor::kStoredDs}) {
+      PlanImage img;
+      plan_image(pr, w, call, true, &img);
+      CHECK(img.off + img.bytes.size() <= w.d_off);
+    }
+    std::vector<int32_t> items, records;
+    plan_items(pr, 1, &items);
+    launch_units(pr, 1, items, {}, &records);
+    UnitList l;
+    split_units(pr, Kernel::kDkdv, records, pr.Hkv, &l);
+    CHECK(l.parts * pr.Hkv <= MAX_PARTS);
+    const bool many = int64_t(records.size()) / kUnitInts * pr.Hkv >= kSplitBelow;
+    if (many && sc.sinks == 0) CHECK(l.units.empty());
+    if (l.units.empty()) continue;
+    split += many;
+    std::vector<int64_t> covered(size_t(l.parts), 0);
+    for (size_t m = 0; m < l.merges.size(); m += kMergeInts) {
+      int64_t tiles = 0, next = 0;
+      for (size_t i = 0; i < records.size(); i += kUnitInts)
+        if (records[i] == l.merges[m])
+          for (int r = 0; r < records[i + 3]; ++r) tiles += (records[i + 6 + 3 * size_t(r)] + KV_QTILE_ROWS - 1) / KV_QTILE_ROWS;
+      for (int32_t part = l.merges[m + 2]; part < l.merges[m + 2] + l.merges[m + 3]; ++part)
+        for (size_t u = 0; u < l.units.size(); u += kUnitInts)
+          if (l.units[u + REC_PART] == part) {
+            CHECK(l.units[u] == l.merges[m] && l.units[u + REC_T0] == next && l.units[u + REC_T1] > next);
+            next = l.units[u + REC_T1];
+            ++covered[size_t(part)];
+          }
+      CHECK(next == tiles);
+    }
+    for (int64_t c : covered) CHECK(c == 1);
+  }
+  if (split < 5) return 1;
   std::printf("%lld pairs, %lld items of two ranges, %lld merged, %lld blocks\n", (long long)pairs_seen, (long long)two_ranges,
               (long long)merged, (long long)blocks);
   return two_ranges > 50 && blocks > 1000 ? 0 : 1;
