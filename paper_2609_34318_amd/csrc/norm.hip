@@ -287,13 +287,12 @@ int hydra_pack_heads_normed_bwd(const hydra_norm_t* p, const void* x, const floa
     prof_end(tok, s);
     if (hipGetLastError() != hipSuccess) return HYDRA_ERR_HIP;
   }
-  if (sums) {
-    const int tok = prof_begin("norm_weights", s);
-    const int rows = p->n_tokens > 0 ? sh.steps * sh.side : 0;
-    hipLaunchKernelGGL(norm_weights_kernel, dim3(unsigned((cols + 63) / 64 * 2)), dim3(kThreads), 0, s, a.part, rows, int(cols),
-                       d_weight, d_bias);
-    prof_end(tok, s);
-  }
+  if (!sums) return HYDRA_OK;
+  const int tok = prof_begin("norm_weights", s);
+  const int rows = p->n_tokens > 0 ? sh.steps * sh.side : 0;
+  hipLaunchKernelGGL(norm_weights_kernel, dim3(unsigned((cols + 63) / 64 * 2)), dim3(kThreads), 0, s, a.part, rows, int(cols),
+                     d_weight, d_bias);
+  prof_end(tok, s);
   return hipGetLastError() == hipSuccess ? HYDRA_OK : HYDRA_ERR_HIP;
 }
 

@@ -615,8 +615,8 @@ def unpack_heads_normed(x, y, weight=None, bias=None, gate=None, center=True, ac
                         stream=None):
     """x [cp_u, T, H/cp_u, d] bf16 -> y [T, H, d] bf16: every head normalised (center: its mean taken off), times weight
     plus bias [H, d] float32, times activation(gate), gate logits [T, H, d] bf16; without a gate, activation of that."""
-    _here(x, y, weight, bias, gate)
     p, n, _, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    _here(x, y, weight, bias, gate)
     _check(lib().hydra_unpack_heads_normed(p, *ins, _ptr(y, "y", _BF16, n), _stream(stream)), "hydra_unpack_heads_normed")
 
 
@@ -625,8 +625,8 @@ def pack_heads_normed_bwd(x, d_y, d_x, weight=None, bias=None, gate=None, d_gate
     """Backward of unpack_heads_normed from its inputs and d_y [T, H, d] bf16: writes d_x (as x), with a gate d_gate, and
     where given d_weight and d_bias [H, d] float32, for which workspace is a uint8 device tensor of
     norm_workspace_size(T, H, d)."""
-    _here(x, d_y, d_x, weight, bias, gate, d_gate, d_weight, d_bias, workspace)
     p, n, cols, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    _here(x, d_y, d_x, weight, bias, gate, d_gate, d_weight, d_bias, workspace)
     _check(lib().hydra_pack_heads_normed_bwd(p, *ins, _ptr(d_y, "d_y", _BF16, n), _ptr(d_x, "d_x", _BF16, n),
                                              _ptr(d_gate, "d_gate", _BF16, n), _ptr(d_weight, "d_weight", _F32, cols),
                                              _ptr(d_bias, "d_bias", _F32, cols), *_scratch(workspace), _stream(stream)),

@@ -120,25 +120,42 @@ def rank_share(lengths: Sequence[int], mb: Sequence[int], gstart: Sequence[int],
 
 
 def problems(share: RankShare, softmax_scale: float = 0.0, softcap: float = 0.0, slopes=None,
-             prefix: Optional[Sequence[int]] = None) -> List[List[hydra.Problem]]:
+             prefix: Optional[Sequence[int]] = None, window: int = 0, sinks: int = 0) -> List[List[hydra.Problem]]:
     """The hydra problems of every sub-share: one per ring step; with modified scores as in scores()."""
     nkv = share.n_kv_heads if share.n_kv_heads != share.n_heads else 0
     out = []
     for p in share.parts:
-        sc = scores(share, p, softcap, slopes, prefix)
+        sc = scores(share, p, softcap, slopes, prefix, window, sinks)
         out.append([hydra.Problem(p.cu, share.n_heads, p.q_segs, st, softmax_scale, n_kv_heads=nkv, scores=sc)
                     for st in p.kv_steps])
     return out
 
 
 def scores(share: RankShare, part: SubShare, softcap: float = 0.0, slopes=None,
-           prefix: Optional[Sequence[int]] = None) -> Optional[hydra.Scores]:
-    """The modified scores of a sub-share from the model's (slopes: one per query head of the model) and the
-    batch's (prefix: one length per sequence of the batch); None where nothing is modified."""
-    if not softcap and slopes is None and prefix is None:
+           prefix: Optional[Sequence[int]] = None, window: int = 0, sinks: int = 0) -> Optional[hydra.Scores]:
+    """The modified scores of a sub-share from the model's (slopes: one per query head of the model; window and sinks)
+    and the batch's (prefix: one length per sequence of the batch); None where nothing is modified."""
+    if not softcap and slopes is None and prefix is None and not window and not sinks:
         return None
     return hydra.Scores(softcap, None if slopes is None else slopes[share.head0:share.head0 + share.n_heads].contiguous(),
-                        None if prefix is None else [prefix[i] for i in part.seqs])
+                        None if prefix is None else [prefix[i] for i in part.seqs], window, sinks)
+
+
+def linear(share: RankShare, part: SubShare, d_k: int = 128, d_v: int = 128, scale: float = 0.0
+           ) -> Tuple[hydra.Linear, List[Tuple[int, int, int]]]:
+    """Linear attention over a sub-share's rows: the problem, whose sequences are the pieces of documents that the rank
+    holds, in the order of their rows, and every piece as (document, its first position there, rows).  A piece starts from
+    the state behind the document's rows before it: that of the piece before, decayed over this piece's rows, plus
+    what this piece adds from zero (linear_fwd without o)."""
+    cu, pieces = part.cu, []
+    for a, n in part.q_segs:
+        for d, (lo, hi) in enumerate(zip(cu[:-1], cu[1:])):
+            x, y = max(a, lo), min(a + n, hi)
+            if y > x:
+                pieces.append((d, x - lo, y - x))
+    edges = np.concatenate([[0], np.cumsum([n for _, _, n in pieces], dtype=np.int64)]) if pieces else np.zeros(2, np.int64)
+    nkv = share.n_kv_heads if share.n_kv_heads != share.n_heads else 0
+    return hydra.Linear(edges, share.n_heads, d_k, d_v, n_kv_heads=nkv, scale=scale), pieces
 
 
 def doc_positions(part: SubShare, segs: Segs) -> np.ndarray:
