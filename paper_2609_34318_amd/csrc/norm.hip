@@ -61,7 +61,7 @@ struct NormArgs {
   const u32x4 *x, *gate, *dy;
   u32x4 *y, *dx, *dgate;
   const float *weight, *bias;
-  float* part;        // [tokens side by side and steps][2][columns]
+  float* part;        // [steps][2][columns]
   int64_t T;
   int cols8;          // columns of 8 channels: H d / 8
   int side;           // tokens side by side in a workgroup
@@ -129,15 +129,30 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
       if (t < a.T) st_stream(dx + t * a.group8, narrow((g - xc * along) * r));
     }
   }
-  if (BWD && a.part) {
-    float* p = a.part + ((int64_t)blockIdx.x * a.side + sub) * 2 * a.cols8 * 8 + col * 8;
-    *reinterpret_cast<f32x8*>(p) = dw;
-    *reinterpret_cast<f32x8*>(p + a.cols8 * 8) = db;
+  if (!BWD || !a.part) return;
+  float* p = a.part + (int64_t)blockIdx.x * 2 * a.cols8 * 8 + col * 8;
+  if (a.side > 1) {  // one row of a workgroup: the tokens side by side added in order, lane `sub` the e-th of 16 values
+    __shared__ float sums[kThreads * 16];
+    const int n = a.cols8, me = sub * n + col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sums[e * kThreads + me] = dw[e];
+      sums[(8 + e) * kThreads + me] = db[e];
+    }
+    __syncthreads();  // threads without a column have ended
+    for (int e = sub; e < 16; e += a.side) {
+      float x = 0.f;
+      for (int i = 0; i < a.side; ++i) x += sums[e * kThreads + i * n + col];
+      p[(e >> 3) * n * 8 + (e & 7)] = x;
+    }
+    return;
   }
+  *reinterpret_cast<f32x8*>(p) = dw;
+  *reinterpret_cast<f32x8*>(p + a.cols8 * 8) = db;
 }
 
-// d_weight and d_bias: the sums of `rows` partial rows.  A workgroup takes 64 columns, 16 lanes of 4 each by 16 rows at
-// a time, and adds the 16 sums in order.
+// d_weight and d_bias: the sums of `rows` partial rows (at most 1024).  A workgroup takes 64 columns, 16 lanes of 4 each
+// by 16 rows at a time, and adds the 16 sums in order.
 __global__ __launch_bounds__(kThreads) void norm_weights_kernel(const float* __restrict__ part, int rows, int cols,
                                                                 float* __restrict__ d_weight, float* __restrict__ d_bias) {
   __shared__ f32x4 sums[16][16];
@@ -145,8 +160,19 @@ __global__ __launch_bounds__(kThreads) void norm_weights_kernel(const float* __r
   const int per = (cols + 63) / 64, which = blockIdx.x / per;
   const int at = (blockIdx.x % per) * 64 + 4 * c;
   f32x4 s = f32x4{};
-  if (at < cols)
-    for (int i = r; i < rows; i += 16) s += *reinterpret_cast<const f32x4*>(part + ((int64_t)i * 2 + which) * cols + at);
+  if (at < cols) {
+    constexpr int AHEAD = 8;  // loads in flight: one after another 1024 rows take 20 us, so 9
+    for (int i0 = r; i0 < rows; i0 += 16 * AHEAD) {
+      f32x4 v[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int i = i0 + 16 * k;
+        v[k] = i < rows ? *reinterpret_cast<const f32x4*>(part + ((int64_t)i * 2 + which) * cols + at) : f32x4{};
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) s += v[k];
+    }
+  }
   sums[r][c] = s;
   __syncthreads();
   float* out = which ? d_bias : d_weight;
@@ -163,16 +189,20 @@ bool sizes_ok(int64_t n_tokens, int32_t n_heads, int32_t d) {
 struct Shape {
   int cols8, side, blocks, steps;  // steps: workgroups along the tokens
 };
-Shape shape_of(int64_t T, int32_t H, int32_t d) {
+// sums: with partial sums, whose rows a workgroup of few tokens would make many of (2K rows x 8 heads of 256: 30 us with 2
+// tokens each).
+constexpr int kSumTokens = 8;
+Shape shape_of(int64_t T, int32_t H, int32_t d, bool sums) {
   Shape s;
   s.cols8 = H * (d / 8);
   s.side = s.cols8 < kThreads ? kThreads / s.cols8 : 1;
   s.blocks = s.side > 1 ? 1 : (s.cols8 + kThreads - 1) / kThreads;
   const int64_t most = std::max(1, 1024 / s.blocks);
-  s.steps = int(std::max<int64_t>(1, std::min<int64_t>(most, (T + s.side - 1) / s.side)));
+  const int64_t tokens = s.side * (sums ? kSumTokens : 1);
+  s.steps = int(std::max<int64_t>(1, std::min<int64_t>(most, (T + tokens - 1) / tokens)));
   return s;
 }
-size_t part_bytes(const Shape& s) { return size_t(s.steps) * size_t(s.side) * 2 * size_t(s.cols8) * 8 * sizeof(float); }
+size_t part_bytes(const Shape& s) { return size_t(s.steps) * 2 * size_t(s.cols8) * 8 * sizeof(float); }
 
 struct Span {
   const void* p;
@@ -242,7 +272,7 @@ int hydra_unpack_heads_normed(const hydra_norm_t* p, const void* x, const float*
     if (misaligned(q)) return HYDRA_ERR_ALIGN;
   const uint64_t cols = uint64_t(p->n_heads) * p->d, n = uint64_t(p->n_tokens) * cols * 2;
   if (outputs_overlap({{y, n}}, {{x, n}, {gate, n}, {weight, cols * 4}, {bias, cols * 4}})) return HYDRA_ERR_INVALID;
-  const Shape sh = shape_of(p->n_tokens, p->n_heads, p->d);
+  const Shape sh = shape_of(p->n_tokens, p->n_heads, p->d, false);
   NormArgs a = args_of(p, sh, x, weight, bias, gate);
   a.y = static_cast<u32x4*>(y);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -253,7 +283,7 @@ int hydra_unpack_heads_normed(const hydra_norm_t* p, const void* x, const float*
 }
 
 size_t hydra_norm_workspace_size(int64_t n_tokens, int32_t n_heads, int32_t d) {
-  return sizes_ok(n_tokens, n_heads, d) ? part_bytes(shape_of(n_tokens, n_heads, d)) : 0;
+  return sizes_ok(n_tokens, n_heads, d) ? part_bytes(shape_of(n_tokens, n_heads, d, true)) : 0;
 }
 
 int hydra_pack_heads_normed_bwd(const hydra_norm_t* p, const void* x, const float* weight, const float* bias,
@@ -267,7 +297,7 @@ int hydra_pack_heads_normed_bwd(const hydra_norm_t* p, const void* x, const floa
                         static_cast<const void*>(d_x), static_cast<const void*>(d_gate), static_cast<const void*>(d_weight),
                         static_cast<const void*>(d_bias)})
     if (misaligned(q)) return HYDRA_ERR_ALIGN;
-  const Shape sh = shape_of(p->n_tokens, p->n_heads, p->d);
+  const Shape sh = shape_of(p->n_tokens, p->n_heads, p->d, sums);
   const size_t need = sums ? part_bytes(sh) : 0;
   if (sums && (!workspace || workspace_bytes < need)) return HYDRA_ERR_WORKSPACE;
   if (sums && misaligned(workspace)) return HYDRA_ERR_ALIGN;
@@ -289,7 +319,7 @@ int hydra_pack_heads_normed_bwd(const hydra_norm_t* p, const void* x, const floa
   }
   if (!sums) return HYDRA_OK;
   const int tok = prof_begin("norm_weights", s);
-  const int rows = p->n_tokens > 0 ? sh.steps * sh.side : 0;
+  const int rows = p->n_tokens > 0 ? sh.steps : 0;
   hipLaunchKernelGGL(norm_weights_kernel, dim3(unsigned((cols + 63) / 64 * 2)), dim3(kThreads), 0, s, a.part, rows, int(cols),
                      d_weight, d_bias);
   prof_end(tok, s);
