@@ -19,7 +19,8 @@
  *   p_j <= p_i  and  (p_i - p_j < w  or  p_j < cu_seqlens[d] + n)
  *
  * (the last w keys up to its own, and the document's first n keys).  What no query of a tile sees is not visited: the
- * work grows with the window.  A ring step whose keys lie behind every window leaves O = 0 and LSE = -inf.  LSE, O, the merge of ring steps and D are those of hydra_attn.h for these
+ * work grows with the window.  A ring step whose keys lie behind every window leaves O = 0 and LSE = -inf; a later one
+ * (merge) and the backward then launch and upload nothing.  LSE, O, the merge of ring steps and D are those of hydra_attn.h for these
  * scores.  Backward, with P = exp(s - LSE) and t = tanh(softmax_scale <q_i, k_j> / c):
  *
  *   dV = P^T dO,  dS = P o (dO V^T - D) o (1 - t^2),  dQ = softmax_scale dS K,  dK = softmax_scale dS^T Q

@@ -316,6 +316,7 @@ int attn_fwd_impl(bool upload, bool merge, const hydra_problem_t* p, const hydra
                          {scratch.at, scratch.bytes}},
                         {{q, qb}, {k, kb}, {v, vb}, {pr.slopes, uint64_t(pr.H) * 4}}))
       return HYDRA_ERR_INVALID;
+    if (merge && !o_bf16 && sees_nothing(pr)) return HYDRA_OK;  // the earlier steps' O and LSE stay as they are
     hipStream_t s = static_cast<hipStream_t>(stream);
     PlanRecord plan;
     if (upload) {  // the forward needs only the query-stationary items
@@ -384,6 +385,7 @@ int attn_bwd_impl(bool upload, const hydra_problem_t* p, const hydra_scores_t* s
                         {{q, qb}, {k, kb}, {v, vb}, {o_final, qh * kDv * uint64_t(o_bytes)}, {lse_final, qh * 4},
                          {d_o, qh * kDv * 2}, {pr.slopes, uint64_t(pr.H) * 4}}))
       return HYDRA_ERR_INVALID;
+    if (sees_nothing(pr)) return HYDRA_OK;  // nothing to add
     hipStream_t s = static_cast<hipStream_t>(stream);
     PlanRecord plan;
     if (upload) {

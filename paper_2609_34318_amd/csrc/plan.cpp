@@ -416,7 +416,10 @@ void split_units(const Problem& pr, Kernel kernel, const std::vector<int32_t>& r
   out->units.swap(sorted);
 }
 
-int64_t visible_pairs(const Problem& pr) {
+namespace {
+
+// Visible pairs of one head; `any`: whether there is one.
+int64_t count_pairs(const Problem& pr, bool any) {
   int64_t total = 0;
   const int n_docs = int(pr.cu.size()) - 1;
   for (int qs = 0; qs < pr.q.n_segs; ++qs) {
@@ -428,6 +431,7 @@ int64_t visible_pairs(const Problem& pr) {
       // documents overlapping the query segment
       int d0 = doc_index(pr.cu, qa), d1 = doc_index(pr.cu, qb - 1);
       for (int d = std::max(d0, 0); d <= d1 && d < n_docs; ++d) {
+        if (any && total > 0) return 1;
         const int64_t da = pr.cu[d], db = pr.cu[d + 1];
         const int64_t q0 = std::max(qa, da), q1 = std::min(qb, db), k0 = std::max(ka, da), k1 = std::min(kb, db);
         if (pr.window > 0) {  // the causal pairs but those behind the window, and of these the sinks
@@ -444,6 +448,11 @@ int64_t visible_pairs(const Problem& pr) {
   }
   return total;
 }
+
+}  // namespace
+
+int64_t visible_pairs(const Problem& pr) { return count_pairs(pr, false); }
+bool sees_nothing(const Problem& pr) { return pr.window > 0 && count_pairs(pr, true) == 0; }
 
 bool ds_path_applies(const Problem& pr) {
   if (pr.nq == 0 || pr.nk == 0) return false;

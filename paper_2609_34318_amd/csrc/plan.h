@@ -44,6 +44,8 @@ int check_problem(const hydra_problem_t* p, const hydra_scores_t* sc, Problem* o
 void plan_items(const Problem& pr, int which, std::vector<int32_t>* items);
 
 int64_t visible_pairs(const Problem& pr);
+// A window's ring step that no query of the rank sees anything of (most steps of a long ring).
+bool sees_nothing(const Problem& pr);
 
 // The kernel a launch list is for: what a tile of its loop costs, and how many it has.
 enum class Kernel { kFwd, kDq, kDkdv };

@@ -177,3 +177,21 @@ def test_plans_of_other_windows_are_refused():
         with pytest.raises(hydra.HydraError) as e:
             hydra.attn_fwd(p, q, k, v, o, lse, ws, planned=True)
         assert e.value.status == -4
+
+
+def test_ring_steps_behind_every_window():
+    """Steps that no row sees anything of change nothing, eager or planned, and need no plan."""
+    s = Setup(([2000], 2, 2, [(1500, 500)], [[(1400, 600)], [(0, 700)], [(700, 700)]]), "window", graph_ready=True)
+    want, sh = s.reference(), s.share()
+    got = s.run(sh)
+    check(s, got, want, "eager")
+    assert not got[6].any() and not got[7].any()  # dK, dV of the second step
+    first = [t.clone() for t in got]
+    ring.plan(sh)
+    assert all(torch.equal(a, b) for a, b in zip(first, s.run(sh, planned=True)))
+    p, (k, v) = sh.problems[1], s.kv[1]
+    assert hydra.visible_pairs(p) == 0
+    hydra.profile_start()
+    hydra.attn_fwd_merge(p, s.q, k, v, sh.o_acc, sh.lse_acc, sh.workspace, planned=True)  # which holds no plan
+    assert hydra.profile_stop() == {}
+    assert torch.equal(sh.o_acc, first[0]) and torch.equal(sh.lse_acc, first[1])
