@@ -63,7 +63,7 @@ typedef struct {
   int32_t sinks;              /* n >= 0                                                        */
 } hydra_scores_t;
 
-/* hydra_workspace_size, hydra_split_scratch_size, hydra_bwd_ds_bytes, hydra_visible_pairs and
+/* hydra_workspace_size, hydra_split_scratch_size (with sinks at most 176 MiB), hydra_bwd_ds_bytes, hydra_visible_pairs and
  * hydra_plan_items of `p` with scores `sc` (host only). */
 size_t hydra_scores_workspace_size(const hydra_problem_t* p, const hydra_scores_t* sc);
 size_t hydra_scores_scratch_size(const hydra_problem_t* p, const hydra_scores_t* sc);

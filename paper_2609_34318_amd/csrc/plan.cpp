@@ -375,7 +375,7 @@ void split_units(const Problem& pr, Kernel kernel, const std::vector<int32_t>& r
     const double beside = heads % 8 == 0 ? all / 32 : all * heads / kCus;
     for (int64_t most = std::max<int64_t>(int64_t(0.75 * beside - cost.group), 2 * kMinPart); most < longest; most += (most + 3) / 4) {
       time_of(most, &parts);
-      if (parts * heads > MAX_PARTS) continue;
+      if (parts * heads > max_parts(pr)) continue;
       best_most = most;
       break;
     }
@@ -384,7 +384,7 @@ void split_units(const Problem& pr, Kernel kernel, const std::vector<int32_t>& r
     const int64_t most = (longest + d - 1) / d;
     if (most < kMinPart) break;
     const double t = time_of(most, &parts) + (ahead.merges ? 0 : cost.merge);
-    if (parts * heads > MAX_PARTS) break;
+    if (parts * heads > max_parts(pr)) break;
     if (t < best) {
       best = t;
       best_most = most;
@@ -521,8 +521,8 @@ WsLayout ws_layout(const Problem& pr, bool noalloc) {
   w.qitems_off = off;
   off = align_up(off + size_t(nqt) * kUnitInts * sizeof(int32_t), 256);
   w.lists_off = off;
-  if (!noalloc)  // what is uneven may be split beside more whole items
-    off += 3 * (kListBytes + (uneven(pr) ? align_up(size_t(std::max(nqt, nkt)) * kUnitInts * sizeof(int32_t), 256) : 0));
+  if (!noalloc)  // what is uneven may be split into more parts, beside more whole items
+    off += 3 * (kListBytes + (uneven(pr) ? align_up(size_t(std::max(nqt, nkt) + MAX_PARTS) * (kUnitInts + kMergeInts) * sizeof(int32_t), 256) : 0));
   w.d_off = off;
   off = align_up(off + size_t(pr.H) * size_t(pr.nq) * sizeof(float), 256);
   w.lse2_off = off;

@@ -70,6 +70,10 @@ constexpr int64_t kSplitBelow = 512;
 // With a window the tile of keys that holds a document's sinks is seen by all of its queries and the others by few: its
 // items are split, however many the launch has, where the longest of them would take longer than all else over the CUs.
 bool uneven(const Problem& pr);
+// Most parts of one launch.  Twice as many with sinks: their own items take many, and where a launch has few workgroups
+// filling the chip takes the others' too (16 query heads on 2, 8K rows, window 4096: dK/dV and its merge 531 us, 664 with
+// 256; window 512: 173 and 182).
+inline int max_parts(const Problem& pr) { return uneven(pr) ? 2 * MAX_PARTS : MAX_PARTS; }
 // The most bytes of a split list: its merges, and a unit for every part and every whole item.
 constexpr size_t kListBytes = (size_t(kMaxMerges) * kMergeInts + size_t(MAX_PARTS + kSplitBelow) * kUnitInts) * sizeof(int32_t);
 static_assert(kListBytes % 256 == 0, "lists end on a region boundary");

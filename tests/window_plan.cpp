@@ -160,7 +160,7 @@ int main() {
     launch_units(pr, 1, items, {}, &records);
     UnitList l;
     split_units(pr, Kernel::kDkdv, records, pr.Hkv, &l);
-    CHECK(l.parts * pr.Hkv <= MAX_PARTS);
+    CHECK(l.parts * pr.Hkv <= max_parts(pr) && (sc.sinks > 0) == (max_parts(pr) > MAX_PARTS));
     const bool many = int64_t(records.size()) / kUnitInts * pr.Hkv >= kSplitBelow;
     if (many && sc.sinks == 0) CHECK(l.units.empty());
     if (l.units.empty()) continue;
