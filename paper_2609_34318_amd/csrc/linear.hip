@@ -15,13 +15,26 @@
 //   S = L^32 S + b^T (weighted c).
 // The MFMA result layout is chosen (rows in the order pi, kernels.h) so that X, and S itself, are operands of the next
 // products as they lie in the registers; a, b and c come through swizzled LDS tiles, b and c by transpose reads too.
-// The next chunk's tiles are copied while one is computed.
+// Later chunks' tiles are copied while one is computed; a wave's rows of y leave through the LDS of its own columns of
+// c, so that a chunk has one barrier.
 //
 // Sequences longer than an item are cut: a first launch (MAIN = false) leaves what each item adds to the state, a scan
 // turns that into the states that the items start from, and the main launch walks every item from its own.
 //
-// Rounding: MFMA operands are bf16.  X and S enter their products as sums of two bf16 values (16 bits), a weighted c as
-// a sum of two, or three (24 bits) where the walk ends in a state that the caller gets.
+// Rounding: MFMA operands are bf16.  A weighted c enters the state as a sum of two bf16 values (16 bits), or three (24
+// bits) where the walk ends in a state that the caller gets.  X and S enter the products for y as one (each term of y
+// then has one rounding of 2^-8 beside the output's own), in the forward as sums of two: what follows o, a norm and
+// its gradients, would carry the difference of o from its own rounding further (a layer's gradients off by 3.8e-3 of
+// their norm instead of 2.4e-3; forward of 16K rows x 16 heads 74 to 82 us).
+//
+// Bound by HBM traffic, some of it beyond the algorithm's: 16K rows x 16 heads of 128 x 128 (rates with the copies
+// of a second read), forward: states 40 us (125 MiB read at 4.1 TB/s; without any computation 37), scan 17, main 88 (289
+// MiB, 3.5 TB/s; without computation 39, of which k and v come from the cache behind the L2); backward: states 70 (4.1
+// TB/s), scan 17, main 184 (702 MiB, 4.0 TB/s).  What the vector unit does per chunk and wave (some 300 instructions, in
+// the forward 500) and the products (34 and 44 of 32 cycles) overlap in part only, with two waves on a SIMD.  Measured and
+// not kept: three waves on a SIMD (registers spill: main 1.4 times slower), priorities around the products and forced
+// orders of products, reads and vector work (the same to 2%), deeper copies than the LDS of two workgroups holds at three
+// stages (the same).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -441,8 +454,9 @@ __global__ __launch_bounds__(256) void lin_group_kernel(Group k, Group v, int gr
 
 // ------------------------------------------------------------------ one token
 // A workgroup takes 32 columns of one row's and head's state: lane group r = tid / 8 its rows r, r + 16, ..., lane
-// tid % 8 four columns.  Bound by the state's bytes.  The first row of a slot takes the later ones too, in order, with
-// the state in its registers.
+// tid % 8 four columns.  Bound by the state's bytes, read and written once in 32 bits (168 rows x 16 heads of 128 x 128:
+// 72 us, 5.0 TB/s); columns in four workgroups also spread a single row over 64 CUs.  The first row of a slot takes the
+// later ones too, in order, with the state in its registers.
 constexpr int STEP_THREADS = 128;
 template <int DK, int DV>
 __global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int n_slots, int H, int Hkv, float scale,
