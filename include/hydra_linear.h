@@ -22,10 +22,10 @@
  *
  * Conventions: those of hydra_attn.h (device pointers unless marked HOST, 16-byte aligned; token-major bf16 tensors;
  * host checks before any HIP call, status codes, streams).  States are fp32 [n_seqs][n_heads][d_k][d_v].  Sums and
- * states are held in 32 bits; the products take weighted scores and states as sums of two bf16 values, and what is
- * added to a state as a sum of three where the state is an output, of two elsewhere.  q, k, v, d_o and the states must
- * be finite: a value that is not reaches rows of its sequence that do not depend on it.  Rows of the tensors from
- * cu_seqlens[n_seqs] on are neither read nor written.
+ * states are held in 32 bits; the products take weighted scores and states as bf16 values, in the forward as sums of two,
+ * and what is added to a state as a sum of three where the state is an output, of two elsewhere.  q, k, v, d_o and the
+ * states must be finite: a value that is not reaches rows of its sequence that do not depend on it.  Rows of the tensors
+ * from cu_seqlens[n_seqs] on are neither read nor written.
  */
 #ifndef HYDRA_LINEAR_H
 #define HYDRA_LINEAR_H
@@ -57,7 +57,8 @@ size_t hydra_linear_workspace_size(const hydra_linear_t* p);
 
 /* Uploads the work plan of `p` into `workspace`, for calls with planned != 0, which only launch kernels (and can be
  * recorded into a graph): they return HYDRA_ERR_WORKSPACE where the workspace does not hold the plan of `p` (strides,
- * scale and d_k, d_v may differ within what the workspace holds), as in hydra_attn.h. */
+ * scale and d_k, d_v may differ within what the workspace holds), as in hydra_attn.h.  While the stream is recorded this
+ * call, and the ones below without `planned`, return it too: the upload's source does not outlive them. */
 int hydra_linear_plan(const hydra_linear_t* p, void* workspace, size_t workspace_bytes, void* stream);
 
 /* q [T][H][d_k], k [T][Hkv][d_k], v [T][Hkv][d_v] bf16 with T = cu_seqlens[n_seqs] rows; decay: float[n_heads] log

@@ -593,6 +593,9 @@ struct Plans {
     return k;
   }
   int upload(void* ws, hipStream_t s) const {
+    hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &recording) != hipSuccess) return HYDRA_ERR_HIP;
+    if (recording != hipStreamCaptureStatusNone) return HYDRA_ERR_WORKSPACE;  // a replay would copy from a freed image
     std::vector<int32_t> image(w.slots_off / sizeof(int32_t), 0);
     for (int i = 0; i < 2; ++i) {
       std::copy(plan[i].items.begin(), plan[i].items.end(), image.begin() + int64_t(w.items_off[i] / sizeof(int32_t)));

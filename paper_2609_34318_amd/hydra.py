@@ -358,6 +358,15 @@ def _ptr(t, what: str = "tensor", dtypes=None, numel: Optional[int] = None) -> O
     instead of reaching a kernel."""
     if t is None:
         return None
+    # one condition in the common case: a small call's time is its checks
+    if not (t.is_cuda and t.is_contiguous() and (dtypes is None or _DTYPE_NAMES.get(t.dtype) in dtypes)
+            and (numel is None or t.numel() == numel)):
+        _refuse(t, what, dtypes, numel)
+    return t.data_ptr()
+
+
+def _refuse(t, what: str, dtypes, numel: Optional[int]):
+    """Raises what _ptr found wrong (nothing where it only had not met the dtype yet)."""
     if not t.is_cuda:
         raise ValueError(f"{what}: a device tensor is required")
     if not t.is_contiguous():
@@ -366,7 +375,6 @@ def _ptr(t, what: str = "tensor", dtypes=None, numel: Optional[int] = None) -> O
         raise ValueError(f"{what}: dtype {t.dtype} is not one of {dtypes}")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
-    return t.data_ptr()
 
 
 _DTYPE_NAMES = {}  # torch dtype -> its name
@@ -681,7 +689,7 @@ def _here(*tensors):
     import torch
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != dev:
+        if t is not None and t.get_device() not in (dev, -1):  # -1: on the host, which the addresses' check refuses
             raise ValueError(f"tensor on device {t.get_device()}, the current device is {dev}")
 
 
@@ -890,7 +898,7 @@ def linear_step(q, k, v, decay, state, o, slots=None, state_out=None, scale: flo
     n, H, d_k = q.shape
     Hk, d_v = v.shape[1], v.shape[2]
     out = state if state_out is None else state_out
-    if tuple(state.shape[1:]) != (H, d_k, d_v) or out.shape != state.shape:
+    if state.shape[1:] != (H, d_k, d_v) or (out is not state and out.shape != state.shape):
         raise ValueError(f"state: shape {tuple(state.shape)}, expected {('n_slots', H, d_k, d_v)}, and state_out the same")
     _check(lib().hydra_linear_step(n, state.shape[0], H, Hk, d_k, d_v, scale, _ptr(q, "q", _BF16),
                                    _ptr(k, "k", _BF16, n * Hk * d_k), _ptr(v, "v", _BF16, n * Hk * d_v),

@@ -132,6 +132,28 @@ def capture(f):
     return graph
 
 
+def test_uploads_are_not_recorded():
+    c = Case([300, 40], 2, 2, 64, 64)
+    hydra.linear_plan(c.p, c.ws)
+    other = torch.empty_like(c.ws)
+
+    def calls():
+        for f in (lambda: hydra.linear_plan(c.p, other), lambda: c.run(planned=False)):
+            with pytest.raises(hydra.HydraError):
+                f()
+        c.run(planned=True)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(3):
+        for t in [c.o, *c.grads]:
+            t.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        near([c.o, c.s_out, *c.grads, c.ds_in], c.reference(), "recorded")
+
+
 @pytest.mark.parametrize("lengths,Hk", [([1, 700, 40], 2), ([64], 4)])
 def test_recorded_calls_replay(lengths, Hk):
     c, eager = Case(lengths, 4, Hk, 64, 64), Case(lengths, 4, Hk, 64, 64)
