@@ -20,7 +20,8 @@
  * with cp_u = 1 the calls are the plain norm.
  *
  * Conventions: those of hydra_gate.h; weight, bias and their gradients are fp32.  Sums are in 32 bits, each bf16 output
- * is rounded once; results are deterministic.
+ * is rounded once; results are deterministic.  x is finite and at most 2^58 in size: the sum of its squares, of up to 512
+ * channels, has to fit 32 bits.  A value that is not finite reaches its own token and head, and the sums d_weight and d_bias.
  */
 #ifndef HYDRA_NORM_H
 #define HYDRA_NORM_H
@@ -57,8 +58,8 @@ int hydra_unpack_heads_normed(const hydra_norm_t* p, const void* x, const float*
 size_t hydra_norm_workspace_size(int64_t n_tokens, int32_t n_heads, int32_t d);
 
 /* Writes d_x [cp_u][T][H/cp_u][d] bf16, d_gate [T][H][d] bf16 (NULL without a gate), and where they are not NULL
- * d_weight and d_bias [H][d] fp32 (d_weight needs weight, d_bias bias).  workspace may be NULL where neither is
- * asked for.  With n_tokens = 0 these two are zero. */
+ * d_weight and d_bias [H][d] fp32 (d_weight needs weight, d_bias bias).  workspace, which the call writes (two that
+ * overlap need one each), may be NULL where neither is asked for.  With n_tokens = 0 these two are zero. */
 int hydra_pack_heads_normed_bwd(const hydra_norm_t* p, const void* x, const float* weight, const float* bias,
                                 const void* gate, const void* d_y, void* d_x, void* d_gate, float* d_weight,
                                 float* d_bias, void* workspace, size_t workspace_bytes, void* stream);

@@ -98,6 +98,28 @@ def test_a_constant_head_and_a_far_mean():
     assert not got["y"].any() and torch.isfinite(got["d_x"].float()).all()
 
 
+@pytest.mark.parametrize("center", [True, False], ids=["center", "rms"])
+def test_values_at_the_ends_of_their_range(center):
+    """Up to 2^58, where the sum of 512 squares still fits 32 bits, and so small that eps alone stands under the root."""
+    x = draw(7, 6, 2, 512, 1, True, True, True, scale=2.0 ** 55)
+    assert 2.0 ** 56 < x["x"].abs().max() <= 2.0 ** 58
+    check(x, run(x, center), center, "silu")
+    x = draw(8, 6, 2, 512, 1, True, True, True, scale=2.0 ** -70)
+    check(x, run(x, center), center, "silu")
+
+
+def test_a_token_that_is_not_finite_stays_by_itself():
+    x = draw(9, 9, 4, 32, 2, True, True, True)
+    want = run(x)
+    x["x"][0, 4, 1, 5], x["x"][1, 7, 0, 0] = float("nan"), float("inf")
+    got = run(x)
+    for n in ("y", "d_gate"):
+        a, b = got[n].float(), want[n].float()
+        other = torch.ones(9, 4, dtype=torch.bool)
+        other[4, 1] = other[7, 2] = False  # head 0 of the second group is head 2
+        assert torch.equal(a[other], b[other]) and not torch.isfinite(a[~other]).any(1).all(), n
+
+
 def test_far_gates():
     x = draw(6, 8, 2, 64, 1, False, False, True)
     x["gate"] = torch.where(torch.rand(x["gate"].shape, generator=torch.Generator().manual_seed(0)) < 0.5, 3e38, -3e38).to(BF16)
