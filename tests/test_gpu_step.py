@@ -75,6 +75,19 @@ def test_parity(dims, H, Hk, how):
     check(x, slots, o, before, c["state"], dk)
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 2600])
+def test_many_rows(n):
+    """Slots of one, of several and of no rows, near each other and far apart."""
+    x = draw(n, n, 700, 1, 1, 64, 64)
+    slots = torch.randint(-50, 750, (n,), generator=torch.Generator().manual_seed(n)).tolist()
+    slots[0] = slots[-1] = slots[n // 2] = 699
+    c = {t: y.cuda() for t, y in x.items()}
+    o = torch.full((n, 1, 64), 7.0, dtype=BF16, device="cuda")
+    before = c["state"].clone()
+    hydra.linear_step(c["q"], c["k"], c["v"], c["decay"], c["state"], o, slots=torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    check(x, slots, o, c["state"], before, 64)
+
+
 def test_steps_continue_a_prompt():
     """The state that a prompt ends with, stepped on, against the whole sequence at once."""
     g = torch.Generator(device="cuda").manual_seed(5)
