@@ -74,6 +74,12 @@ __device__ __forceinline__ float log2_decay(const float* decay, int head) {
   return fmax2(__int_as_float(((cint*)decay)[head]) * LOG2E, -1.0e30f);
 }
 
+// w x, and 0 for x = 0 whatever w: the weights of a short chunk's rows that do not exist (zeros in LDS) may have grown past
+// 32 bits where those of its own rows have not.  One instruction, as the product (weights of these rows held at 0 and the
+// whole chunks' formed anew behind a short one: up to 37 registers spilled).  The compiler has no builtin for it.
+extern "C" __device__ float hydra_fmul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float weighted(float x, float w) { return hydra_fmul_legacy(x, w); }
+
 // x as bf16, and what that leaves of it (the pairs' bits, so that a value is converted once)
 __device__ __forceinline__ bf16x8 split_bf16(float (&x)[8]) {
   const bf16x8 hi = to_bf16x8(x);
@@ -276,7 +282,7 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
     for (int s = 0; s < 2; ++s) {
       float c8[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c8[e] = (float)cf[s][e] * (wu[8 * s + e] * per_unit);
+      for (int e = 0; e < 8; ++e) c8[e] = weighted((float)cf[s][e], wu[8 * s + e] * per_unit);
 #pragma unroll
       for (int i = 0; i < PARTS - 1; ++i) part[s][i] = split_bf16(c8);
       part[s][PARTS - 1] = to_bf16x8(c8);
@@ -303,7 +309,7 @@ __device__ __forceinline__ void lin_walk(const Walk& w, const Common& cm, int it
       for (int s = 0; s < 2; ++s) {
         float p[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = x[8 * s + e] * wx[8 * s + e];
+        for (int e = 0; e < 8; ++e) p[e] = weighted(x[8 * s + e], wx[8 * s + e]);
         if constexpr (REST) y = mfma(cf[s], split_bf16(p), y);
         y = mfma(cf[s], to_bf16x8(p), y);
       }
