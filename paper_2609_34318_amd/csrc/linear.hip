@@ -463,7 +463,9 @@ __global__ __launch_bounds__(256) void lin_group_kernel(Group k, Group v, int gr
 // tid % 8 four columns.  Bound by the state's bytes, read and written once in 32 bits (168 rows x 16 heads of 128 x 128:
 // 72 us, 5.0 TB/s); columns in four workgroups also spread a single row over 64 CUs.  The first row of a slot takes the
 // later ones too, in order, with the state in its registers; a workgroup reads all slots for that, once where no slot is
-// there twice (4096 rows x 4 heads of 64 x 64: 110 us, 81 without slots; 1024 rows: 23 and 22).
+// there twice: work that grows with the square of the rows (4096 rows x 4 heads of 64 x 64: 115 us, 89 without slots; 1024
+// rows: 30 and 29; 64K rows x 1 head: 1.42 ms and 0.44).  A repeated slot's next row is looked for up to the first 1024 rows
+// that hold one, so that n rows of one slot are n times the same work (1.2 us each; a search to the last row took 5 of 32K).
 constexpr int STEP_THREADS = 128;
 template <int DK, int DV>
 __global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int n_slots, int H, int Hkv, float scale,
@@ -486,8 +488,8 @@ __global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int 
   for (int i = 0; i < NR; ++i) S[i] = *reinterpret_cast<const f32x4*>(state + at + i * 16 * DV);
   constexpr int NO_ROW = 0x7fffffff;
   int next = NO_ROW;  // the slot's next row, of those that this lane looks at
-  // f(row) of the rows from `first` on that have the slot, 1024 rows at a time
-  auto each_row = [&](int first, auto f) {
+  // f(row) of the rows from `first` on that have the slot, 1024 rows at a time; with `stop` up to the 1024 that have one
+  auto each_row = [&](int first, bool stop, auto f) {
     for (int b = first; b < n_rows; b += 8 * STEP_THREADS) {
       int at[8];
       if (b + 8 * STEP_THREADS <= n_rows) {
@@ -505,11 +507,12 @@ __global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int 
         for (int u = 0; u < 8; ++u)
           if (at[u] == slot) f(b + tid + u * STEP_THREADS);
       }
+      if (stop && __syncthreads_or(any)) break;
     }
   };
   if (slots) {
     int earlier = 0;
-    each_row(0, [&](int b) {
+    each_row(0, false, [&](int b) {
       earlier |= b < row;
       if (b > row) next = min(next, b);
     });
@@ -551,7 +554,7 @@ __global__ __launch_bounds__(STEP_THREADS) void lin_step_kernel(int n_rows, int 
     if (next == NO_ROW) break;
     row = next;
     next = NO_ROW;
-    each_row(row + 1, [&](int b) { next = min(next, b); });
+    each_row(row + 1, true, [&](int b) { next = min(next, b); });
     __syncthreads();  // part and next_row are read
   }
 #pragma unroll
