@@ -273,7 +273,7 @@ class Scores:
 
     @property
     def any(self) -> bool:
-        return self.softcap != 0 or self.slopes is not None or self.prefix is not None or self.window != 0
+        return self.softcap != 0 or self.slopes is not None or self.prefix is not None or self.window != 0 or self.sinks != 0
 
 
 class Problem:

@@ -97,3 +97,10 @@ def test_the_window_is_part_of_the_plan():
     a, b = _problem(window=300, sinks=4), _problem(window=300, sinks=4, softcap=30.0)
     assert hydra.workspace_size(a) == hydra.workspace_size(b)
     assert all(np.array_equal(hydra.plan_items(a, w), hydra.plan_items(b, w)) for w in (0, 1))
+
+
+def test_sinks_alone_are_no_plain_problem():
+    """Sinks without a window are refused by every call, and by the one that has no modified scores too."""
+    assert hydra.Scores(sinks=3).any and not hydra.Scores().any
+    with pytest.raises(ValueError, match="modified scores"):
+        hydra.attn_bwd_noalloc(_problem(sinks=3), *[None] * 9)
