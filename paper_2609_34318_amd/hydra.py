@@ -377,6 +377,17 @@ def _refuse(t, what: str, dtypes, numel: Optional[int]):
         raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
 
 
+def _shaped(t, what: str, dtypes, shape: Tuple[int, ...]) -> Optional[int]:
+    """_ptr of a tensor of one shape: as many elements in another order would be read as if they lay in this one."""
+    if t is None:
+        return None
+    if not (t.shape == shape and t.is_cuda and t.is_contiguous() and _DTYPE_NAMES.get(t.dtype) in dtypes):
+        if t.shape != shape:
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+        _refuse(t, what, dtypes, None)
+    return t.data_ptr()
+
+
 _DTYPE_NAMES = {}  # torch dtype -> its name
 
 
@@ -613,31 +624,37 @@ def _norm(x, weight, bias, gate, center: bool, activation: str, eps: float):
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation {activation!r}: one of {ACTIVATIONS} is required")
     cp_u, T, Hg, d = x.shape
-    H, n = cp_u * Hg, x.numel()
+    H = cp_u * Hg
     p = NormC(n_tokens=T, n_heads=H, d=d, cp_u=cp_u, center=int(bool(center)), activation=ACTIVATIONS.index(activation), eps=eps)
-    return ctypes.byref(p), n, H * d, (_ptr(x, "x", _BF16), _ptr(weight, "weight", _F32, H * d), _ptr(bias, "bias", _F32, H * d),
-                                       _ptr(gate, "gate", _BF16, n))
+    return ctypes.byref(p), (T, H, d), (_ptr(x, "x", _BF16), _channels(weight, "weight", H, d), _channels(bias, "bias", H, d),
+                                        _shaped(gate, "gate", _BF16, (T, H, d)))
+
+
+def _channels(t, what: str, H: int, d: int) -> Optional[int]:
+    """Address of float32 values per head and channel, [H, d] or one row of them."""
+    return _shaped(t, what, _F32, (H * d,) if t is not None and t.dim() == 1 else (H, d))
 
 
 def unpack_heads_normed(x, y, weight=None, bias=None, gate=None, center=True, activation="silu", eps: float = 1e-5,
                         stream=None):
     """x [cp_u, T, H/cp_u, d] bf16 -> y [T, H, d] bf16: every head normalised (center: its mean taken off), times weight
-    plus bias [H, d] float32, times activation(gate), gate logits [T, H, d] bf16; without a gate, activation of that."""
-    p, n, _, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    plus bias [H, d] (or [H * d]) float32, times activation(gate), gate logits [T, H, d] bf16; without a gate, activation of
+    that."""
+    p, rows, ins = _norm(x, weight, bias, gate, center, activation, eps)
     _here(x, y, weight, bias, gate)
-    _check(lib().hydra_unpack_heads_normed(p, *ins, _ptr(y, "y", _BF16, n), _stream(stream)), "hydra_unpack_heads_normed")
+    _check(lib().hydra_unpack_heads_normed(p, *ins, _shaped(y, "y", _BF16, rows), _stream(stream)), "hydra_unpack_heads_normed")
 
 
 def pack_heads_normed_bwd(x, d_y, d_x, weight=None, bias=None, gate=None, d_gate=None, d_weight=None, d_bias=None,
                           workspace=None, center=True, activation="silu", eps: float = 1e-5, stream=None):
     """Backward of unpack_heads_normed from its inputs and d_y [T, H, d] bf16: writes d_x (as x), with a gate d_gate, and
-    where given d_weight and d_bias [H, d] float32, for which workspace is a uint8 device tensor of
+    where given d_weight and d_bias [H, d] (or [H * d]) float32, for which workspace is a uint8 device tensor of
     norm_workspace_size(T, H, d)."""
-    p, n, cols, ins = _norm(x, weight, bias, gate, center, activation, eps)
+    p, rows, ins = _norm(x, weight, bias, gate, center, activation, eps)
     _here(x, d_y, d_x, weight, bias, gate, d_gate, d_weight, d_bias, workspace)
-    _check(lib().hydra_pack_heads_normed_bwd(p, *ins, _ptr(d_y, "d_y", _BF16, n), _ptr(d_x, "d_x", _BF16, n),
-                                             _ptr(d_gate, "d_gate", _BF16, n), _ptr(d_weight, "d_weight", _F32, cols),
-                                             _ptr(d_bias, "d_bias", _F32, cols), *_scratch(workspace), _stream(stream)),
+    _check(lib().hydra_pack_heads_normed_bwd(p, *ins, _shaped(d_y, "d_y", _BF16, rows), _shaped(d_x, "d_x", _BF16, x.shape),
+                                             _shaped(d_gate, "d_gate", _BF16, rows), _channels(d_weight, "d_weight", *rows[1:]),
+                                             _channels(d_bias, "d_bias", *rows[1:]), *_scratch(workspace), _stream(stream)),
            "hydra_pack_heads_normed_bwd")
 
 
@@ -816,8 +833,12 @@ class Linear:
         return ctypes.byref(self.c)
 
     @property
+    def state_shape(self) -> Tuple[int, int, int, int]:
+        return self.n_seqs, self.n_heads, self.d_k, self.d_v
+
+    @property
     def state_numel(self) -> int:
-        return self.n_seqs * self.n_heads * self.d_k * self.d_v
+        return math.prod(self.state_shape)
 
 
 def linear_workspace_size(p: Linear) -> int:
@@ -865,9 +886,9 @@ def linear_fwd(p: Linear, q, k, v, decay, o, workspace, state_in=None, state_out
     _here(q, k, v, decay, o, workspace, state_in, state_out)
     qp, kp, vp = _linear_rows(p, q, k, v)
     _check(lib().hydra_linear_fwd(p.ref, qp, kp, vp, _ptr(decay, "decay", _F32, p.n_heads),
-                                  _ptr(state_in, "state_in", _F32, p.state_numel),
+                                  _shaped(state_in, "state_in", _F32, p.state_shape),
                                   _dense_rows(o, "o", p.n_tokens, p.n_heads, p.d_v),
-                                  _ptr(state_out, "state_out", _F32, p.state_numel), _ptr(workspace, "workspace"),
+                                  _shaped(state_out, "state_out", _F32, p.state_shape), _ptr(workspace, "workspace"),
                                   workspace.numel() * workspace.element_size(), int(planned), _stream(stream)),
            "hydra_linear_fwd")
 
@@ -880,11 +901,11 @@ def linear_bwd(p: Linear, q, k, v, decay, d_o, dq, dk, dv, workspace, state_in=N
     qp, kp, vp = _linear_rows(p, q, k, v)
     T, H, Hk = p.n_tokens, p.n_heads, p.n_kv_heads
     _check(lib().hydra_linear_bwd(p.ref, qp, kp, vp, _ptr(decay, "decay", _F32, H),
-                                  _ptr(state_in, "state_in", _F32, p.state_numel), _dense_rows(d_o, "d_o", T, H, p.d_v),
-                                  _ptr(d_state_out, "d_state_out", _F32, p.state_numel),
+                                  _shaped(state_in, "state_in", _F32, p.state_shape), _dense_rows(d_o, "d_o", T, H, p.d_v),
+                                  _shaped(d_state_out, "d_state_out", _F32, p.state_shape),
                                   _dense_rows(dq, "dq", T, H, p.d_k), _dense_rows(dk, "dk", T, Hk, p.d_k),
                                   _dense_rows(dv, "dv", T, Hk, p.d_v),
-                                  _ptr(d_state_in, "d_state_in", _F32, p.state_numel), _ptr(workspace, "workspace"),
+                                  _shaped(d_state_in, "d_state_in", _F32, p.state_shape), _ptr(workspace, "workspace"),
                                   workspace.numel() * workspace.element_size(), int(planned), _stream(stream)),
            "hydra_linear_bwd")
 
@@ -901,9 +922,9 @@ def linear_step(q, k, v, decay, state, o, slots=None, state_out=None, scale: flo
     if state.shape[1:] != (H, d_k, d_v) or (out is not state and out.shape != state.shape):
         raise ValueError(f"state: shape {tuple(state.shape)}, expected {('n_slots', H, d_k, d_v)}, and state_out the same")
     _check(lib().hydra_linear_step(n, state.shape[0], H, Hk, d_k, d_v, scale, _ptr(q, "q", _BF16),
-                                   _ptr(k, "k", _BF16, n * Hk * d_k), _ptr(v, "v", _BF16, n * Hk * d_v),
+                                   _shaped(k, "k", _BF16, (n, Hk, d_k)), _shaped(v, "v", _BF16, (n, Hk, d_v)),
                                    _ptr(decay, "decay", _F32, H), _ptr(state, "state", _F32), _ptr(out, "state_out", _F32),
-                                   _ptr(slots, "slots", ("int32",), n), _ptr(o, "o", _BF16, n * H * d_v),
+                                   _ptr(slots, "slots", ("int32",), n), _shaped(o, "o", _BF16, (n, H, d_v)),
                                    _stream(stream)), "hydra_linear_step")
 
 
