@@ -21,7 +21,8 @@
  *
  * Conventions: those of hydra_gate.h; weight, bias and their gradients are fp32.  Sums are in 32 bits, each bf16 output
  * is rounded once; results are deterministic.  x is finite and at most 2^58 in size: the sum of its squares, of up to 512
- * channels, has to fit 32 bits.  A value that is not finite reaches its own token and head, and the sums d_weight and d_bias.
+ * channels, has to fit 32 bits.  A value that is not finite reaches no other token and head than its own but through the
+ * sums over tokens: d_weight, and d_bias, in which x has no part where there is a gate.
  */
 #ifndef HYDRA_NORM_H
 #define HYDRA_NORM_H

@@ -127,3 +127,44 @@ def test_far_gates():
     y, _, _, z = oracle.forward(oracle.unpack(x["x"].double()), gate=x["gate"].double().numpy(), activation="sigmoid")
     assert np.abs(got["y"].double().cpu().numpy() - y).max() <= 2.0 ** -8 * np.abs(y).max()
     assert not got["d_gate"].any()
+
+
+@pytest.mark.parametrize("gate", [True, False], ids=["gate", "plain"])
+def test_where_a_value_that_is_not_finite_goes(gate):
+    """x: its token and head (every channel) and d_weight, d_bias only where the activation is of the norm itself; d_y: its
+    own channel's d_gate, its token and head of d_x, and both sums of its channel."""
+    x = draw(11, 9, 4, 32, 2, True, True, gate)
+    want = run(x)
+    bad = {n: None if t is None else t.clone() for n, t in x.items()}
+    bad["x"][0, 4, 1, 5], bad["x"][1, 7, 0, 0] = float("nan"), float("inf")
+    got = run(bad)
+    heads = torch.zeros(9, 4, dtype=torch.bool)
+    heads[4, 1] = heads[7, 2] = True  # head 0 of the second group is head 2
+
+    def flat(t, n):
+        t = t.float().cpu()
+        return torch.cat(list(t), 1) if n == "d_x" else t
+    for n in ("y", "d_gate", "d_x"):
+        if got[n] is not None:
+            a, b = flat(got[n], n), flat(want[n], n)
+            assert torch.equal(a[~heads], b[~heads]) and not torch.isfinite(a[heads]).any(), n
+    of_head = heads.any(0)
+    for n in ("d_weight", "d_bias"):
+        a, b = got[n].cpu(), want[n].cpu()
+        assert torch.equal(a[~of_head], b[~of_head]), n
+        if n == "d_bias" and gate:  # the sum of d_y act(gate): x has no part in it
+            assert torch.equal(a, b)
+        else:
+            assert not torch.isfinite(a[of_head]).any(), n
+    bad = {n: None if t is None else t.clone() for n, t in x.items()}
+    bad["d_y"][3, 2, 7] = float("nan")
+    got = run(bad)
+    assert torch.equal(got["y"], want["y"])
+    heads[:] = False
+    heads[3, 2] = True
+    a, b = flat(got["d_x"], "d_x"), flat(want["d_x"], "d_x")
+    assert torch.equal(a[~heads], b[~heads]) and not torch.isfinite(a[heads]).any()
+    for n in ("d_weight", "d_bias"):
+        assert torch.isfinite(got[n]).sum() == 4 * 32 - 1 and not torch.isfinite(got[n][2, 7]), n
+    if gate:
+        assert torch.isfinite(got["d_gate"]).sum() == 9 * 4 * 32 - 1 and not torch.isfinite(got["d_gate"][3, 2, 7])
