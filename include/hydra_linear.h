@@ -62,8 +62,8 @@ size_t hydra_linear_workspace_size(const hydra_linear_t* p);
 int hydra_linear_plan(const hydra_linear_t* p, void* workspace, size_t workspace_bytes, void* stream);
 
 /* q [T][H][d_k], k [T][Hkv][d_k], v [T][Hkv][d_v] bf16 with T = cu_seqlens[n_seqs] rows; decay: float[n_heads] log
- * decays, 4-byte aligned, read when the kernels run (-infinity forgets at once; above 0 states grow, and e^(g n) over the
- * n rows of a sequence has to fit 32 bits, n = 1 in hydra_linear_step).
+ * decays, 4-byte aligned, read when the kernels run (-infinity forgets at once; above 0 states grow, and
+ * e^(g n) over the n rows of a sequence has to fit 32 bits, n = 1 in hydra_linear_step).
  *   o          [T][H][d_v] bf16, or NULL: only the last states are computed
  *   state_in   NULL (zero), or the states that the sequences start from
  *   state_out  NULL, or receives their last states; may be state_in itself

@@ -27,14 +27,15 @@
 // its gradients, would carry the difference of o from its own rounding further (a layer's gradients off by 3.8e-3 of
 // their norm instead of 2.4e-3; forward of 16K rows x 16 heads 74 to 82 us).
 //
-// Bound by HBM traffic, some of it beyond the algorithm's: 16K rows x 16 heads of 128 x 128 (rates with the copies
-// of a second read), forward: states 40 us (125 MiB read at 4.1 TB/s; without any computation 37), scan 17, main 88 (289
-// MiB, 3.5 TB/s; without computation 39, of which k and v come from the cache behind the L2); backward: states 70 (4.1
-// TB/s), scan 17, main 184 (702 MiB, 4.0 TB/s).  What the vector unit does per chunk and wave (some 300 instructions, in
-// the forward 500) and the products (34 and 44 of 32 cycles) overlap in part only, with two waves on a SIMD.  Measured and
-// not kept: three waves on a SIMD (registers spill: main 1.4 times slower), priorities around the products and forced
-// orders of products, reads and vector work (the same to 2%), deeper copies than the LDS of two workgroups holds at three
-// stages (the same).
+// 16K rows x 16 heads of 128 x 128 (profiler, 200 passes; rates with the copies of a second read), forward: states 36 us
+// (4.6 TB/s; 37 without any computation), scan 15, main 75 (289 MiB, 4.05 TB/s); backward: states 59 (4.8 TB/s), scan 15, main
+// 156 (722 MiB, 4.85 TB/s), where a copy of 1 GiB runs at 5.15.  All but one are bound by HBM traffic, some of it beyond the
+// algorithm's.  The forward's main launch is not: without computation it takes 39 us (k and v then come from the cache behind
+// the L2).  What bounds it is a chunk's chain of dependent work at two waves a SIMD (1.4 on average): the matrix units are
+// busy for 32% of the cycles (52 products of 32 cycles a chunk and wave), the vector unit for 49% (some 500 instructions),
+// which overlap in part only, and a wave waits for 21% of its time.  (Backward: 35%, 44%, 26%.)  Measured and not kept: three
+// waves on a SIMD (registers spill: main 1.4 times slower), priorities around the products and forced orders of products,
+// reads and vector work (the same to 2%), deeper copies than the LDS of two workgroups holds at three stages (the same).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -10,8 +10,12 @@ namespace {
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Workgroups that a walk is cut into: two run on each of 256 CUs.  The three walks of the backward make 1.5 times as
-// many of half the number, and its states and their scan cost more (16K rows x 16 heads of 128 x 128: forward 143 us in
-// 512 items, 164 in 336, 154 in 256; backward 284, 264, 249, and 243 in 170).
+// many of half the number, and its states and their scan cost more.  16K rows x 16 heads of 128 x 128: forward 143 us in
+// 512 items, 164 in 336, 154 in 256 (one run); backward (another run) 251 in 512, 250 in 384, 228 in 256, 223 in 170 and 128.
+// The backward takes 256 because of ten shapes of 2K to 64K rows it is within 8% of the best number on nine: 512 is 10 to
+// 29% slower than it on six; 170 is 7% faster on 4K rows x 32 heads and 2 to 5% on three others, but 19% slower on 32K x 16 of
+// 64 x 64, 5% on 16K x 16 of 128 x 64, and 28% on eight documents of 1000 rows x 16 (138 us; 108 in 256, and 79 in 128,
+// which leaves them whole).
 constexpr int64_t kLinearGroups[2] = {512, 256};
 // The fewest rows of an item of a cut sequence (2K rows in four documents x 8 heads of 64 x 64: forward 26 us, 33 with 256).
 constexpr int64_t kLinearMinRows = 128;

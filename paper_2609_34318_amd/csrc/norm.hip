@@ -1,7 +1,7 @@
 // The norm of every head with an activation or a gate, fused with the exchange's unpack (hydra_norm.h).
 //
 // Both calls are bound by HBM: forward 6 bytes per element with a gate, backward 10, each read or written once (16K
-// tokens x 64 heads of 128: 150 us, 5.3 TB/s, and 265 us, 5.0 TB/s, sums of weights 4).  A lane
+// tokens x 64 heads of 128, profiler: 155 us, 5.2 TB/s, and 273 us, 5.0 TB/s, sums of weights 5).  A lane
 // owns 8 channels (16 bytes) of one head for all of its tokens, so that weight and bias, and in the backward the sums of
 // their gradients, stay in its registers; the d / 8 lanes of a head are neighbours in one wave and sum by butterfly.  A
 // workgroup has 256 such columns, or where a token has fewer several tokens side by side, and takes every `step`-th
@@ -24,7 +24,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256;
-// Tokens of a lane at a time (16K tokens x 64 heads of 128: backward 265 us, 290 with four, which hold a third fewer waves).
+// Tokens of a lane at a time (16K tokens x 64 heads of 128, events around it: backward 274 us, 296 with four, which hold a
+// third fewer waves; forward 161 and 166).
 constexpr int kUnroll = 2;
 
 __device__ __forceinline__ u32x4 ld_stream(const u32x4* p) { return __builtin_nontemporal_load(p); }

@@ -14,8 +14,8 @@ namespace hydra {
 // bound what any of its rows sees.  With a window a query also sees the keys before its lo at less than `sinks` from
 // its document's start, and of keys hi does not grow: a sink is seen to its document's end (span_min, span_max).
 // The window costs what its edges cost: tiles at either end of a row's window evaluate the mask, and a tile of 256 rows
-// walks 255 keys more than a row (16K rows x 8 heads, cap 50, window 4096: forward 383 us, 800 TFLOP/s of visible pairs
-// against 870 of the whole mask; dK/dV 751, dQ from dS 277).  Below some 500 keys the kernels are bound by their rows:
+// walks 255 keys more than a row (16K rows x 8 heads, cap 50, window 4096: forward 373 us, 820 TFLOP/s of visible pairs
+// against 870 of the whole mask; dK/dV 736, dQ from dS 278).  Below some 500 keys the kernels are bound by their rows:
 // accumulators read and written, O in two types (8K rows x 16 heads, window 128: forward 59 us, 45 of it bytes).
 struct Span {
   int lo, hi, start;  // start: of the document
